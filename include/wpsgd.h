@@ -291,6 +291,119 @@ int wpsgd_shard_indices(uint64_t seed, int chain, int k, int64_t n0, int64_t cou
 int wpsgd_shard_indices_device(uint64_t seed, int chain, int k, int64_t n0, int64_t count, int64_t m,
                                int64_t *out_device, void *stream);
 
+/* ---- a linear model with many classes (the output layer of a language model), trained by the same workers ----
+ * A class vector for every class, scores z = W x, the softmax loss, one clipped and regularised step over all of a worker's
+ * tensors, and answers drawn from the scores.  The workers' tensors are averaged with wpsgd_weights and wpsgd_combine.
+ * None of these calls takes HOST arrays unless it says so, so they can be recorded into a HIP graph.                  */
+
+/* A matrix in 8-bit floating point, a power of two for each block of 128 elements of a row:
+ *   value(i, c) = codes[i*ld + c] (as e4m3) * 2^(exps[i*ld_exps + c/128] - 127)
+ * Rows hold whole blocks: codes of columns cols .. 128*ceil(cols/128)-1 are 0 (a product reads them).              */
+typedef struct wpsgd_blocks {
+    int64_t rows, cols;        /* 0 <= cols <= 2^31                                                       */
+    void *codes;               /* DEVICE, one byte each, 16-byte aligned                                  */
+    int64_t ld;                /* row stride in bytes, a multiple of 16, >= 128*ceil(cols/128)            */
+    void *exps;                /* DEVICE, one byte for each block, 4-byte aligned                         */
+    int64_t ld_exps;           /* row stride in bytes, a multiple of 4, >= ceil(cols/128)                 */
+} wpsgd_blocks;
+
+/* Rows of the data set X (dense; CSR: UNSUPPORTED) in that form.  For a block whose largest finite size is s the power is the least
+ * 2^e with s <= 448 * 2^e (e >= -126; 1 for a block of zeros), and a code the nearest e4m3 value, half to even.
+ * What is not finite becomes NaN.
+ *   rows       DEVICE, n row numbers, such as wpsgd_sample_indices_device writes; one outside [0, m) stands for a row of zeros.
+ *              NULL: rows 0 .. n-1
+ *   transpose  0: out is n x d, blocks along d.  Not 0: out is d x n, blocks along the n rows.
+ *   out        its rows and cols say so; codes and exps are written, the padding of codes with 0 (not the padding of exps)
+ * Errors: INVALID_ARG, UNSUPPORTED (CSR; more than 2^31 - 1 workgroups), HIP_ERROR.                                    */
+int wpsgd_quantize(const wpsgd_matrix *X, const int64_t *rows, int64_t n, int transpose, const wpsgd_blocks *out, void *stream);
+
+/* out[i*ld_out + j] = sum_c A(i, c) * B(j, c), for all rows i of A and j of B: summed in fp32, rounded once to dtype.
+ * With x the rows of a batch (n x d), W the class vectors (classes x d) and G the loss gradient (n x classes):
+ *   scores              A = x, B = W                 gradient of W      A = G transposed, B = x transposed
+ *   gradient of x       A = G, B = W transposed      (transposed: as wpsgd_quantize makes it)
+ *   out        DEVICE, A->rows x B->rows; it may not overlap A or B
+ *   workspace  DEVICE scratch of at least wpsgd_block_matmul_workspace(A->rows, B->rows, A->cols) bytes, 256-byte aligned
+ *              (may be NULL where that is 0)
+ * The result does not depend on timing.  Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, UNSUPPORTED, HIP_ERROR.              */
+size_t wpsgd_block_matmul_workspace(int64_t rows_a, int64_t rows_b, int64_t cols);
+int wpsgd_block_matmul(const wpsgd_blocks *A, const wpsgd_blocks *B, void *out, int64_t ld_out, wpsgd_dtype dtype,
+                       void *workspace, size_t workspace_bytes, void *stream);
+
+/* Softmax cross-entropy of n rows of scores, and its gradient:
+ *   loss[i]    = r_i * (log sum_c exp(z_ic) - z_i,label)
+ *   grad[i, c] = scale * r_i * (softmax(z_i)_c - [c = label_i])          the gradient of scale * sum_i loss[i]
+ * A row with a negative label or r_i = 0 does not count: loss and gradient are 0 whatever its scores.  A row whose scores
+ * are all -inf has loss +inf and gradient 0.  A label >= classes makes the row's loss and gradient NaN.
+ *   Z            DEVICE, n x classes, row stride ld elements, fp32 or bfloat16
+ *   labels       DEVICE, n                    row_weights  DEVICE, n (r_i), or NULL for ones
+ *   loss         DEVICE out, n fp32           grad         DEVICE out, dtype as Z, row stride ld_grad; NULL: not wanted.
+ *                                             It may be Z itself (with ld_grad = ld), else it may not overlap it.
+ *   workspace    DEVICE scratch of at least wpsgd_softmax_loss_workspace(...) bytes, 256-byte aligned (NULL where that is 0)
+ * Statistics are fp32; the result does not depend on timing.  Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, HIP_ERROR.      */
+size_t wpsgd_softmax_loss_workspace(int64_t n, int64_t classes, wpsgd_dtype dtype);
+int wpsgd_softmax_loss(const void *Z, int64_t n, int64_t classes, int64_t ld, wpsgd_dtype dtype, const int64_t *labels,
+                       const float *row_weights, double scale, float *loss, void *grad, int64_t ld_grad,
+                       void *workspace, size_t workspace_bytes, void *stream);
+
+/* A model that lies in many tensors: gradients in fp32 or bfloat16, weights in fp32.  A list is made once from HOST
+ * descriptions (this call copies them, so it cannot be recorded into a graph; the others can) and stays valid while the
+ * tensors stay where they are.  `table` is DEVICE memory of wpsgd_tensor_list_bytes(...), 256-byte aligned, that belongs to
+ * the list from then on.  wpsgd_tensor_list_bytes returns 0 for arguments the call would refuse.                   */
+typedef struct wpsgd_tensor {
+    void *grad;                /* DEVICE, n elements of dtype                                             */
+    float *weight;             /* DEVICE, n elements, or NULL in a list that no step is taken on          */
+    int64_t n;                 /* >= 0                                                                    */
+    wpsgd_dtype dtype;
+} wpsgd_tensor;
+typedef struct wpsgd_tensor_list {      /* filled in by wpsgd_tensor_list_make */
+    const void *table;
+    int64_t chunks, elements;
+    int has_weights;
+} wpsgd_tensor_list;
+size_t wpsgd_tensor_list_bytes(const wpsgd_tensor *tensors, int64_t count);
+int wpsgd_tensor_list_make(const wpsgd_tensor *tensors, int64_t count, void *table, size_t table_bytes,
+                           wpsgd_tensor_list *list, void *stream);
+
+/* norm = sqrt(sum of the squares of all gradients), summed in fp64: no square of an fp32 value overflows.  norm is DEVICE,
+ * one fp32; all three calls write it, and none depends on timing.
+ *   wpsgd_clip_grads     g <- g * max_norm / norm  where norm is finite and over max_norm; else nothing is written
+ *   wpsgd_clipped_step   w <- (1 - eta*lambda) * w - eta * min(1, max_norm / norm) * g   (g stays as it is); a norm that
+ *                        is not finite changes no weight.  max_norm may be infinite: no clipping.
+ *   workspace  DEVICE scratch of at least wpsgd_grad_norm_workspace(list) bytes, 256-byte aligned
+ * Errors: INVALID_ARG (eta, lambda as for wpsgd_run_chains; max_norm > 0), WORKSPACE_TOO_SMALL, HIP_ERROR.              */
+size_t wpsgd_grad_norm_workspace(const wpsgd_tensor_list *list);
+int wpsgd_grad_norm(const wpsgd_tensor_list *list, float *norm, void *workspace, size_t workspace_bytes, void *stream);
+int wpsgd_clip_grads(const wpsgd_tensor_list *list, double max_norm, float *norm, void *workspace, size_t workspace_bytes,
+                     void *stream);
+int wpsgd_clipped_step(const wpsgd_tensor_list *list, double eta, double lambda, double max_norm, float *norm,
+                       void *workspace, size_t workspace_bytes, void *stream);
+
+/* One class drawn for each of n rows of scores.  Classes stand in order of score, the lower index first among equals (NaN
+ * counts as -inf, and -inf is never drawn).  Kept are the first top_k (<= 0: all), of those the ones whose weight is at
+ * least min_p times the largest, and of those the shortest run from the front that holds top_p of their weight (>= 1: all;
+ * at least one class).  With q_c = floor(2^((z_c - max) * log2(e) / temperature) * 2^31 + 1/2) and Q the sum over what is kept, the
+ * answer is the first kept class, by index, at which the sum of q passes floor(u * Q).  Weights and sums are whole numbers: the same row gets the
+ * same answer however many rows or compute units a call has.  temperature 0: the largest score (lowest index).
+ * A field row_x, DEVICE with n entries, stands in for x where it is not NULL.                                           */
+typedef struct wpsgd_draw_rule {
+    float temperature;
+    int top_k;
+    float top_p, min_p;
+    const float *row_temperature;
+    const int32_t *row_top_k;
+    const float *row_top_p, *row_min_p;
+} wpsgd_draw_rule;
+/*   Z        DEVICE, n x classes, row stride ld elements, fp32 or bfloat16; classes <= 2^24
+ *   u        DEVICE, n numbers in [0, 1)
+ *   drawn    DEVICE out, n; -1 for a row without a class that can be drawn
+ *   probs    DEVICE out, n, or NULL: q / Q of the class drawn (0 beside -1)
+ *   workspace DEVICE scratch of at least wpsgd_draw_classes_workspace(...) bytes, 256-byte aligned (NULL where that is 0)
+ * Errors: INVALID_ARG (temperature >= 0, min_p <= 1, neither NaN), WORKSPACE_TOO_SMALL, HIP_ERROR.                      */
+size_t wpsgd_draw_classes_workspace(int64_t n, int64_t classes, wpsgd_dtype dtype);
+int wpsgd_draw_classes(const void *Z, int64_t n, int64_t classes, int64_t ld, wpsgd_dtype dtype, const float *u,
+                       const wpsgd_draw_rule *rule, int64_t *drawn, float *probs,
+                       void *workspace, size_t workspace_bytes, void *stream);
+
 /* ---- diagnostics ---- */
 /* Streaming ceiling probe (not a step of the method): `groups` workgroups of 256 threads each read
  * `rows_per_group` rows of the dense matrix X, in the order the sample stream of chain = group index

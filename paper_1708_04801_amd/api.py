@@ -30,6 +30,10 @@ EXPORTS = [
     "wpsgd_run_chains_from", "wpsgd_shard_indices", "wpsgd_shard_indices_device",
     "wpsgd_run_spans_workspace", "wpsgd_run_spans", "wpsgd_span_condition", "wpsgd_objective_static",
     "wpsgd_chains_status", "wpsgd_run_delay_chains_workspace", "wpsgd_run_delay_chains",
+    "wpsgd_quantize", "wpsgd_block_matmul_workspace", "wpsgd_block_matmul",
+    "wpsgd_softmax_loss_workspace", "wpsgd_softmax_loss", "wpsgd_tensor_list_bytes", "wpsgd_tensor_list_make",
+    "wpsgd_grad_norm_workspace", "wpsgd_grad_norm", "wpsgd_clip_grads", "wpsgd_clipped_step",
+    "wpsgd_draw_classes_workspace", "wpsgd_draw_classes",
 ]
 
 
@@ -44,6 +48,25 @@ class _CPlan(ctypes.Structure):
                 ("prefetch", ctypes.c_int), ("state_in_hbm", ctypes.c_int),
                 ("rows", ctypes.c_int), ("helpers", ctypes.c_int), ("slices", ctypes.c_int),
                 ("slice_wait_us", ctypes.c_int)]
+
+
+class _CBlocks(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("codes", ctypes.c_void_p), ("ld", ctypes.c_int64),
+                ("exps", ctypes.c_void_p), ("ld_exps", ctypes.c_int64)]
+
+
+class _CTensor(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int)]
+
+
+class _CTensorList(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("chunks", ctypes.c_int64), ("elements", ctypes.c_int64), ("has_weights", ctypes.c_int)]
+
+
+class _CDrawRule(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_float), ("top_k", ctypes.c_int), ("top_p", ctypes.c_float), ("min_p", ctypes.c_float),
+                ("row_temperature", ctypes.c_void_p), ("row_top_k", ctypes.c_void_p), ("row_top_p", ctypes.c_void_p),
+                ("row_min_p", ctypes.c_void_p)]
 
 
 class WpsgdError(RuntimeError):
@@ -100,6 +123,25 @@ def load():
     L.wpsgd_objective_workspace.restype = sz
     L.wpsgd_objective.argtypes = [pm, vp, vp, f64, ci, vp, vp, sz, vp]
     L.wpsgd_objective_static.argtypes = [pm, vp, vp, f64, ci, vp, vp]
+    pb, pl, pt = ctypes.POINTER(_CBlocks), ctypes.POINTER(_CTensorList), ctypes.POINTER(_CTensor)
+    L.wpsgd_quantize.argtypes = [pm, vp, i64, ci, pb, vp]
+    L.wpsgd_block_matmul_workspace.argtypes = [i64, i64, i64]
+    L.wpsgd_block_matmul_workspace.restype = sz
+    L.wpsgd_block_matmul.argtypes = [pb, pb, vp, i64, ci, vp, sz, vp]
+    L.wpsgd_softmax_loss_workspace.argtypes = [i64, i64, ci]
+    L.wpsgd_softmax_loss_workspace.restype = sz
+    L.wpsgd_softmax_loss.argtypes = [vp, i64, i64, i64, ci, vp, vp, f64, vp, vp, i64, vp, sz, vp]
+    L.wpsgd_tensor_list_bytes.argtypes = [pt, i64]
+    L.wpsgd_tensor_list_bytes.restype = sz
+    L.wpsgd_tensor_list_make.argtypes = [pt, i64, vp, sz, pl, vp]
+    L.wpsgd_grad_norm_workspace.argtypes = [pl]
+    L.wpsgd_grad_norm_workspace.restype = sz
+    L.wpsgd_grad_norm.argtypes = [pl, vp, vp, sz, vp]
+    L.wpsgd_clip_grads.argtypes = [pl, f64, vp, vp, sz, vp]
+    L.wpsgd_clipped_step.argtypes = [pl, f64, f64, f64, vp, vp, sz, vp]
+    L.wpsgd_draw_classes_workspace.argtypes = [i64, i64, ci]
+    L.wpsgd_draw_classes_workspace.restype = sz
+    L.wpsgd_draw_classes.argtypes = [vp, i64, i64, i64, ci, vp, ctypes.POINTER(_CDrawRule), vp, vp, vp, sz, vp]
     _lib = L
     return L
 
@@ -471,3 +513,219 @@ def wpsgd_stream_rows(X: Matrix, groups, rows_per_group, seed=0, stream=None) ->
     if rc != OK:
         raise WpsgdError(rc, "wpsgd_stream_rows")
     return sink
+
+
+# ---- a linear model with many classes ----
+
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+@dataclass
+class BlockMatrix:
+    """rows x cols in 8-bit floating point, a power of two for each block of 128 elements of a row:
+    codes float8_e4m3fn [rows, whole blocks] with zeros behind the last column, exps uint8 [rows, blocks, padded to whole words],
+    value = code * 2^(exp - 127).  wpsgd_quantize makes one."""
+    rows: int
+    cols: int
+    codes: torch.Tensor
+    exps: torch.Tensor
+
+    def c_struct(self) -> _CBlocks:
+        codes, exps = self.codes, self.exps
+        assert codes.is_cuda and exps.is_cuda and codes.element_size() == 1 and exps.dtype == torch.uint8
+        assert codes.dim() == 2 and exps.dim() == 2 and codes.shape[0] == self.rows and exps.shape[0] == self.rows
+        blocks = -(-self.cols // 128)
+        assert codes.shape[1] >= 128 * blocks and exps.shape[1] >= blocks
+        assert self.rows == 0 or self.cols == 0 or (codes.stride(1) == 1 and exps.stride(1) == 1)
+        return _CBlocks(self.rows, self.cols, codes.data_ptr(), codes.stride(0), exps.data_ptr(), exps.stride(0))
+
+
+def _call_workspace(workspace, need, device, stream):
+    """The caller's workspace, or a temporary one, as address and size."""
+    if workspace is None:
+        if not need:
+            return None, 0
+        workspace = _workspace(need, device, stream)
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def wpsgd_quantize(X: Matrix, rows: Optional[torch.Tensor] = None, transpose=False, codes: Optional[torch.Tensor] = None,
+                   exps: Optional[torch.Tensor] = None, stream=None) -> BlockMatrix:
+    """Rows of a dense data set (all, or those that `rows`, int64 on the GPU, names) as a BlockMatrix, blocks along the
+    columns; transpose=True: one row for each column of X, blocks along the rows taken."""
+    cm = X.c_struct()
+    if rows is not None:
+        assert rows.is_cuda and rows.dtype == torch.int64 and rows.is_contiguous()
+        n = rows.numel()
+    else:
+        n = X.m
+    r, c = (X.d, n) if transpose else (n, X.d)
+    blocks = -(-c // 128)
+    if codes is None:
+        assert X.dense is not None
+        codes = torch.empty((r, 128 * blocks), dtype=torch.float8_e4m3fn, device=X.dense.device)
+    if exps is None:
+        exps = torch.empty((r, -(-blocks // 4) * 4), dtype=torch.uint8, device=codes.device)
+    out = BlockMatrix(r, c, codes, exps)
+    rc = load().wpsgd_quantize(ctypes.byref(cm), rows.data_ptr() if rows is not None else None, n, int(bool(transpose)),
+                               ctypes.byref(out.c_struct()), _stream(stream))
+    if rc != OK:
+        raise WpsgdError(rc, "wpsgd_quantize")
+    return out
+
+
+def wpsgd_block_matmul_workspace(rows_a, rows_b, cols) -> int:
+    return int(load().wpsgd_block_matmul_workspace(int(rows_a), int(rows_b), int(cols)))
+
+
+def wpsgd_block_matmul(A: BlockMatrix, B: BlockMatrix, out: Optional[torch.Tensor] = None, dtype=torch.bfloat16,
+                       workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """out[i, j] = sum_c A[i, c] B[j, c], float32 or bfloat16."""
+    if out is None:
+        out = torch.empty((A.rows, B.rows), dtype=dtype, device=A.codes.device)
+    assert out.is_cuda and out.dtype in _DTYPES and out.shape == (A.rows, B.rows) and (out.numel() == 0 or out.stride(1) == 1)
+    L = load()
+    p, size = _call_workspace(workspace, L.wpsgd_block_matmul_workspace(A.rows, B.rows, A.cols), out.device, stream)
+    rc = L.wpsgd_block_matmul(ctypes.byref(A.c_struct()), ctypes.byref(B.c_struct()), out.data_ptr(), max(out.stride(0), B.rows),
+                              _DTYPES[out.dtype], p, size, _stream(stream))
+    if rc != OK:
+        raise WpsgdError(rc, "wpsgd_block_matmul")
+    return out
+
+
+def _rows_of(Z):
+    assert Z.is_cuda and Z.dim() == 2 and Z.dtype in _DTYPES and (Z.numel() == 0 or Z.stride(1) == 1)
+    return Z.shape[0], Z.shape[1], (Z.stride(0) if Z.shape[0] > 1 else max(Z.stride(0), Z.shape[1]))
+
+
+def wpsgd_softmax_loss_workspace(n, classes, dtype) -> int:
+    return int(load().wpsgd_softmax_loss_workspace(int(n), int(classes), _DTYPES[dtype]))
+
+
+def wpsgd_softmax_loss(Z: torch.Tensor, labels: torch.Tensor, scale=1.0, row_weights: Optional[torch.Tensor] = None,
+                       loss: Optional[torch.Tensor] = None, grad=True, workspace: Optional[torch.Tensor] = None, stream=None):
+    """(loss, grad): the rows' weighted cross-entropies (float32) and the gradient of scale * sum(loss) with respect to
+    the scores Z, in Z's type.  grad: True for a new tensor, a tensor to write (Z itself too), or False for none."""
+    n, c, ld = _rows_of(Z)
+    assert labels.is_cuda and labels.dtype == torch.int64 and labels.is_contiguous() and labels.numel() == n
+    if row_weights is not None:
+        assert row_weights.is_cuda and row_weights.dtype == torch.float32 and row_weights.is_contiguous() and row_weights.numel() == n
+    if loss is None:
+        loss = torch.empty(n, dtype=torch.float32, device=Z.device)
+    assert loss.is_cuda and loss.dtype == torch.float32 and loss.is_contiguous() and loss.numel() == n
+    if grad is True:
+        grad = torch.empty((n, c), dtype=Z.dtype, device=Z.device)
+    g_ptr, g_ld = None, 0
+    if grad is not False and grad is not None:
+        gn, gc, g_ld = _rows_of(grad)
+        assert grad.dtype == Z.dtype and (gn, gc) == (n, c)
+        g_ptr = grad.data_ptr()
+    else:
+        grad = None
+    L = load()
+    dt = _DTYPES[Z.dtype]
+    p, size = _call_workspace(workspace, L.wpsgd_softmax_loss_workspace(n, c, dt), Z.device, stream)
+    rc = L.wpsgd_softmax_loss(Z.data_ptr(), n, c, ld, dt, labels.data_ptr(), row_weights.data_ptr() if row_weights is not None else None,
+                              float(scale), loss.data_ptr(), g_ptr, g_ld, p, size, _stream(stream))
+    if rc != OK:
+        raise WpsgdError(rc, "wpsgd_softmax_loss")
+    return loss, grad
+
+
+class TensorList:
+    """A model that lies in many tensors, as the calls below take it.  Holds on to the tensors; stays valid while they stay in place."""
+
+    def __init__(self, grads, weights, table, c_list):
+        self.grads, self.weights, self.table, self.c_list = grads, weights, table, c_list
+
+
+def wpsgd_tensor_list(grads, weights=None, stream=None) -> TensorList:
+    """Gradients (float32 or bfloat16) and, for steps, the weights (float32) of the same sizes; all contiguous, on one GPU."""
+    grads = list(grads)
+    weights = list(weights) if weights is not None else None
+    assert weights is None or len(weights) == len(grads)
+    items = (_CTensor * max(len(grads), 1))()
+    device = grads[0].device if grads else torch.device("cuda", torch.cuda.current_device())
+    for i, g in enumerate(grads):
+        assert g.is_cuda and g.device == device and g.dtype in _DTYPES and g.is_contiguous()
+        w = weights[i] if weights is not None else None
+        if w is not None:
+            assert w.device == device and w.dtype == torch.float32 and w.is_contiguous() and w.numel() == g.numel()
+        items[i] = _CTensor(g.data_ptr(), w.data_ptr() if w is not None else None, g.numel(), _DTYPES[g.dtype])
+    L = load()
+    need = L.wpsgd_tensor_list_bytes(items, len(grads))
+    table = _workspace(need, device, stream)
+    c_list = _CTensorList()
+    rc = L.wpsgd_tensor_list_make(items, len(grads), table.data_ptr(), table.numel(), ctypes.byref(c_list), _stream(stream))
+    if rc != OK:
+        raise WpsgdError(rc, "wpsgd_tensor_list_make")
+    return TensorList(grads, weights, table, c_list)
+
+
+def wpsgd_grad_norm_workspace(tensors: TensorList) -> int:
+    return int(load().wpsgd_grad_norm_workspace(ctypes.byref(tensors.c_list)))
+
+
+def _norm_call(name, tensors, args, norm, workspace, stream):
+    L = load()
+    if norm is None:
+        norm = torch.empty((), dtype=torch.float32, device=tensors.table.device)
+    assert norm.is_cuda and norm.dtype == torch.float32 and norm.numel() == 1
+    c_list = ctypes.byref(tensors.c_list)
+    p, size = _call_workspace(workspace, L.wpsgd_grad_norm_workspace(c_list), norm.device, stream)
+    rc = getattr(L, name)(c_list, *args, norm.data_ptr(), p, size, _stream(stream))
+    if rc != OK:
+        raise WpsgdError(rc, name)
+    return norm
+
+
+def wpsgd_grad_norm(tensors: TensorList, norm: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """The norm of all the list's gradients together (one float32 on the GPU)."""
+    return _norm_call("wpsgd_grad_norm", tensors, (), norm, workspace, stream)
+
+
+def wpsgd_clip_grads(tensors: TensorList, max_norm, norm: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                     stream=None) -> torch.Tensor:
+    """Scales the gradients in place to a norm of at most max_norm; returns the norm they had."""
+    return _norm_call("wpsgd_clip_grads", tensors, (float(max_norm),), norm, workspace, stream)
+
+
+def wpsgd_clipped_step(tensors: TensorList, eta, lam, max_norm=float("inf"), norm: Optional[torch.Tensor] = None,
+                       workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """weights <- (1 - eta lam) weights - eta min(1, max_norm / norm) gradients, in place; returns the gradients' norm."""
+    return _norm_call("wpsgd_clipped_step", tensors, (float(eta), float(lam), float(max_norm)), norm, workspace, stream)
+
+
+def wpsgd_draw_classes_workspace(n, classes, dtype) -> int:
+    return int(load().wpsgd_draw_classes_workspace(int(n), int(classes), _DTYPES[dtype]))
+
+
+def wpsgd_draw_classes(Z: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
+                       drawn: Optional[torch.Tensor] = None, probs: Optional[torch.Tensor] = None,
+                       workspace: Optional[torch.Tensor] = None, stream=None):
+    """(drawn, probs): a class for each row of the scores Z (int64, -1 where none can be drawn) and its probability among
+    the classes that were kept (float32).  u: float32 in [0, 1).  Each setting is a number, or a tensor with one for each row (float32; top_k int32)."""
+    n, c, ld = _rows_of(Z)
+    assert u.is_cuda and u.dtype == torch.float32 and u.is_contiguous() and u.numel() == n
+    rule = _CDrawRule(1.0, 0, 1.0, 0.0)
+    for name, v, dt in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32),
+                        ("min_p", min_p, torch.float32)):
+        if isinstance(v, torch.Tensor):
+            assert v.is_cuda and v.dtype == dt and v.is_contiguous() and v.numel() == n
+            setattr(rule, "row_" + name, v.data_ptr())
+        else:
+            setattr(rule, name, v)
+    if drawn is None:
+        drawn = torch.empty(n, dtype=torch.int64, device=Z.device)
+    if probs is None:
+        probs = torch.empty(n, dtype=torch.float32, device=Z.device)
+    assert drawn.is_cuda and drawn.dtype == torch.int64 and drawn.is_contiguous() and drawn.numel() == n
+    assert probs.is_cuda and probs.dtype == torch.float32 and probs.is_contiguous() and probs.numel() == n
+    L = load()
+    dt = _DTYPES[Z.dtype]
+    p, size = _call_workspace(workspace, L.wpsgd_draw_classes_workspace(n, c, dt), Z.device, stream)
+    rc = L.wpsgd_draw_classes(Z.data_ptr(), n, c, ld, dt, u.data_ptr(), ctypes.byref(rule), drawn.data_ptr(), probs.data_ptr(), p, size,
+                              _stream(stream))
+    if rc != OK:
+        raise WpsgdError(rc, "wpsgd_draw_classes")
+    return drawn, probs

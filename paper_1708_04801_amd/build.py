@@ -39,6 +39,11 @@ UNITS = [
     ("chain_dense_octet", "chain_dense_octet.hip", []),
     ("chain_delay", "chain_delay.hip", []),
     ("chain_csr", "chain_csr.hip", []),
+    ("block_quantize", "block_quantize.hip", []),
+    ("block_matmul", "block_matmul.hip", []),
+    ("softmax_loss", "softmax_loss.hip", []),
+    ("tensor_step", "tensor_step.hip", []),
+    ("draw_classes", "draw_classes.hip", []),
     ("chain_csr_pair", "chain_csr_pair.hip", []),
     ("chain_dense_reg_f32_hinge", "chain_dense_reg.hip", ["-DWPSGD_TX_BF16=0", "-DWPSGD_LOSS=0"]),
     ("chain_dense_reg_f32_logistic", "chain_dense_reg.hip", ["-DWPSGD_TX_BF16=0", "-DWPSGD_LOSS=1"]),

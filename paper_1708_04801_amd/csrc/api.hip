@@ -26,7 +26,7 @@ bool dense_reg_shape_bf16_loss1(int, int, int);
 
 static thread_local int g_last_hip_error = 0;
 
-static int hip_fail(hipError_t e)
+int hip_fail(hipError_t e)
 {
     g_last_hip_error = (int)e;
     return WPSGD_HIP_ERROR;
@@ -52,7 +52,7 @@ static bool dense_reg_shape(int dtype, int loss, int threads, int ept, int vec)
 
 static size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
 
-static int check_matrix(const wpsgd_matrix *X)
+int check_matrix(const wpsgd_matrix *X)
 {
     if (!X) return WPSGD_INVALID_ARG;
     if (X->m < 1 || X->m > 0xFFFFFFFFLL || X->d < 1) return WPSGD_INVALID_ARG;
@@ -470,7 +470,7 @@ static int upload_filled(void *dst, size_t bytes, hipStream_t s, F &&fill)
     return WPSGD_OK;
 }
 
-static int upload(void *dst, const void *src, size_t bytes, hipStream_t s)
+int upload(void *dst, const void *src, size_t bytes, hipStream_t s)
 {
     return upload_filled(dst, bytes, s, [&](void *host) { std::memcpy(host, src, bytes); });
 }

@@ -99,6 +99,13 @@ __host__ __device__ inline int delay_team_size(int64_t n, int64_t share)
     return members < 1 ? 1 : members > kDelayTeamMax ? kDelayTeamMax : (int)members;
 }
 
+// Notes the failed HIP call for wpsgd_last_hip_error; returns WPSGD_HIP_ERROR.
+int hip_fail(hipError_t e);
+// Copies bytes of host memory to the device through a pinned staging buffer, queued on the stream; the source may be reused at once.
+int upload(void *dst, const void *src, size_t bytes, hipStream_t s);
+int check_matrix(const wpsgd_matrix *X);
+int check_blocks(const wpsgd_blocks *q);
+
 enum class Family { DenseReg, DenseMem, Csr };
 
 // A fully resolved plan (every field chosen).

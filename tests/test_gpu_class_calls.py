@@ -1,0 +1,85 @@
+"""The many-class operators as a program calls them: on other streams, in a HIP graph, one behind the other."""
+import pytest
+import torch
+
+from paper_1708_04801_amd import api
+
+pytestmark = pytest.mark.gpu
+
+
+class Step:
+    """one worker's step with all its buffers made beforehand"""
+
+    def __init__(self, n=70, classes=300, d=200, seed=0):
+        g = torch.Generator().manual_seed(seed)
+        self.x = torch.randn(500, d, generator=g).bfloat16().cuda()
+        self.rows = torch.randint(0, 500, (n,), generator=g).cuda()
+        self.labels = torch.randint(0, classes, (n,), generator=g).cuda()
+        self.W0 = (torch.randn(classes, d, generator=g) * 0.1).cuda()
+        self.W = self.W0.clone()
+        self.u = torch.rand(n, generator=g).cuda()
+        self.dW = torch.empty_like(self.W)
+        self.tensors = api.wpsgd_tensor_list([self.dW.view(-1)], [self.W.view(-1)])
+        torch.cuda.synchronize()
+
+    def __call__(self, stream=None):
+        X = api.Matrix(500, self.x.shape[1], dense=self.x)
+        W = api.Matrix(self.W.shape[0], self.W.shape[1], dense=self.W)
+        x, w = api.wpsgd_quantize(X, rows=self.rows, stream=stream), api.wpsgd_quantize(W, stream=stream)
+        Z = api.wpsgd_block_matmul(x, w, stream=stream)
+        drawn, probs = api.wpsgd_draw_classes(Z, self.u, top_k=20, top_p=0.9, stream=stream)
+        loss, G = api.wpsgd_softmax_loss(Z, self.labels, scale=1.0 / len(self.rows), stream=stream)
+        g = api.wpsgd_quantize(api.Matrix(G.shape[0], G.shape[1], dense=G), transpose=True, stream=stream)
+        xt = api.wpsgd_quantize(X, rows=self.rows, transpose=True, stream=stream)
+        api.wpsgd_block_matmul(g, xt, out=self.dW, stream=stream)
+        norm = api.wpsgd_clipped_step(self.tensors, 0.5, 1e-3, 0.05, stream=stream)
+        self.keep = (x, w, Z, G, g, xt)
+        return drawn, probs, loss, norm
+
+    def result(self, out):
+        torch.cuda.synchronize()
+        return [t.clone() for t in out] + [self.W.clone()]
+
+
+def test_another_stream_gives_the_same_bits():
+    s = Step()
+    want = s.result(s())
+    s.W.copy_(s.W0)
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        out = s()
+    stream.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, s.result(out)))
+    s.W.copy_(s.W0)
+    torch.cuda.synchronize()
+    out = s(stream=stream)                            # named, while another stream is current
+    stream.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, s.result(out)))
+
+
+def test_a_graph_of_the_whole_step_replays():
+    s = Step(seed=1)
+    s()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    s.W.copy_(s.W0)
+    with torch.cuda.graph(graph):
+        out = s()
+    for _ in range(4):
+        s.W.copy_(s.W0)
+        torch.cuda.synchronize()
+        want = s.result(s())                          # eager work of the program's own between the replays
+        s.W.copy_(s.W0)
+        for t in out:
+            t.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(want, s.result(out)))
+
+
+def test_steps_bring_the_loss_down():
+    """the whole batch's loss is convex and a step of length 0.025 against its gradient lowers it, each time"""
+    s = Step(seed=2)
+    losses = [float(s()[2].double().mean()) for _ in range(30)]
+    assert all(b < a for a, b in zip(losses, losses[1:]))

@@ -393,7 +393,7 @@ typedef struct wpsgd_draw_rule {
     const int32_t *row_top_k;
     const float *row_top_p, *row_min_p;
 } wpsgd_draw_rule;
-/*   Z        DEVICE, n x classes, row stride ld elements, fp32 or bfloat16; classes <= 2^24
+/*   Z        DEVICE, n x classes, row stride ld elements, fp32 or bfloat16; classes <= 2^18 (more: UNSUPPORTED)
  *   u        DEVICE, n numbers in [0, 1)
  *   drawn    DEVICE out, n; -1 for a row without a class that can be drawn
  *   probs    DEVICE out, n, or NULL: q / Q of the class drawn (0 beside -1)

@@ -51,7 +51,7 @@ def test_draws_are_the_definitions(n, c, pad, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("c", [33000, 131072, 140001])
+@pytest.mark.parametrize("c", [33000, 131072, 140001, 1 << 18])
 def test_long_rows(c, dtype):
     z = whole_scores(2, c, dtype, c)
     g = torch.Generator().manual_seed(c)
@@ -95,6 +95,16 @@ def test_masked_rows(c, dtype):
     for rule in RULES:
         drawn, probs = check(z, torch.rand(12, generator=g).cuda(), rule)
         assert drawn[0] == drawn[1] == -1 and not probs[:2].any() and drawn[2] == c - 1 and drawn[7] == 3 and drawn[11] == 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("c,low", [(3000, 2), (30000, 1), (60000, 3)])
+def test_scores_with_hardly_a_difference(c, low, dtype):
+    """thousands of ties at the end of the run: more than a list holds"""
+    z = whole_scores(3, c, dtype, c + low, low=low)
+    g = torch.Generator().manual_seed(c)
+    for rule in RULES + [dict(top_k=c - 1), dict(top_k=c // 2, top_p=0.7), dict(top_k=1024), dict(top_k=1025, top_p=0.3, min_p=0.5)]:
+        check(z, torch.rand(3, generator=g).cuda(), rule)
 
 
 def test_settings_of_each_row_its_own():
@@ -180,6 +190,9 @@ def test_refusals():
             bad()
     drawn, _ = api.wpsgd_draw_classes(z[:0], u[:0])
     assert drawn.numel() == 0
+    with pytest.raises(api.WpsgdError) as e:
+        api.wpsgd_draw_classes(torch.zeros(1, (1 << 18) + 1, device="cuda"), u[:1])
+    assert e.value.status == api.UNSUPPORTED
     # settings of rows cannot be refused: a temperature that is no positive number is 0, a min_p over 1 is 1
     drawn, _ = api.wpsgd_draw_classes(z, u + 0.9, temperature=torch.tensor([-1.0, math.nan, 1.0], device="cuda"),
                                       min_p=torch.tensor([0.0, 0.0, 7.0], device="cuda"))

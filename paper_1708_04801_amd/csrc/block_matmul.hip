@@ -20,6 +20,7 @@ struct MatmulArgs {
     int blocks;
     void *out;
     int64_t ldo;
+    int each;                  // blocks to a part of the sum (all, where it is not split)
 };
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -44,65 +45,118 @@ __device__ inline void store4(uint16_t *p, const f32x4 &v)
     *(global_ptr<any_words2>)p = words2{bf16_pack(v[0], v[1]), bf16_pack(v[2], v[3])};
 }
 
-// 64 x 64 results to a workgroup, 32 x 32 to a wave, operands straight from memory.
-template <typename TO>
-__global__ __launch_bounds__(256) void matmul_simple_kernel(MatmulArgs g)
+// Few rows against many.  The one operand's rows (the class vectors of a serving call) are read once, straight from memory into the matrix instructions, sixteen
+// rows times NT to a wave; the other's 16 MT rows come from the caches with every block.  kWaves waves to a workgroup: `along` of them share the blocks of the
+// sum and add up through LDS, in their order, the others take the next rows.  Bound by memory: 16 x 65536 x 4096 reads 268 MB.
+// `turned`: the many rows are A's (results of a lane lie below each other), else B's (beside each other).
+constexpr int kRowWaves = 8;
+template <int MT, int NT, typename TO>
+__global__ __launch_bounds__(64 * kRowWaves) void matmul_rows_kernel(MatmulArgs g, int along, bool turned)
 {
+    __shared__ f32x4 sums[kRowWaves][MT * NT][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t tiles = (g.N + 63) / 64;
-    const int64_t tm = (int64_t)blockIdx.x / tiles, tn = (int64_t)blockIdx.x - tm * tiles;
-    const int64_t i0 = tm * 64 + (wave >> 1) * 32, j0 = tn * 64 + (wave & 1) * 32;
-    const int r = lane & 15, k = (lane >> 4) * 32;
-    const uint8_t *pa[2], *pb[2], *sa[2], *sb[2];
+    const uint8_t *many = turned ? g.a : g.b, *few = turned ? g.b : g.a, *many_e = turned ? g.ea : g.eb, *few_e = turned ? g.eb : g.ea;
+    const int64_t ld_many = turned ? g.lda : g.ldb, ld_few = turned ? g.ldb : g.lda, lde_many = turned ? g.lde_a : g.lde_b, lde_few = turned ? g.lde_b : g.lde_a;
+    const int64_t rows_many = turned ? g.M : g.N, rows_few = turned ? g.N : g.M;
+    const int across = kRowWaves / along, mine = wave % along;
+    const int64_t s0 = ((int64_t)blockIdx.x * across + wave / along) * (16 * NT), h0 = (int64_t)blockIdx.y * (16 * MT);
+    const int r = lane & 15, group = lane >> 4;
+    const int each = (g.blocks + along - 1) / along;
+    const int first = mine * each, last = first + each < g.blocks ? first + each : g.blocks;
+    f32x4 acc[MT][NT];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        const int64_t i = i0 + t * 16 + r < g.M ? i0 + t * 16 + r : g.M - 1, j = j0 + t * 16 + r < g.N ? j0 + t * 16 + r : g.N - 1;
-        pa[t] = g.a + i * g.lda + k;
-        pb[t] = g.b + j * g.ldb + k;
-        sa[t] = g.ea + i * g.lde_a;
-        sb[t] = g.eb + j * g.lde_b;
-    }
-    f32x4 acc[2][2];
+    for (int t = 0; t < MT; ++t)
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+        for (int u = 0; u < NT; ++u) acc[t][u] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (s0 < rows_many) {
+        const uint8_t *ps[NT], *es[NT], *ph[MT], *eh[MT];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) acc[t][u] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int b = 0; b < g.blocks; ++b) {
-        uint4 fa[2][2], fb[2][2];
-        float ca[2], cb[2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                fa[t][h] = *reinterpret_cast<const uint4 *>(pa[t] + (int64_t)b * 128 + h * 16);
-                fb[t][h] = *reinterpret_cast<const uint4 *>(pb[t] + (int64_t)b * 128 + h * 16);
-            }
-            ca[t] = power_of(sa[t][b]);
-            cb[t] = power_of(sb[t][b]);
+        for (int u = 0; u < NT; ++u) {
+            const int64_t i = s0 + u * 16 + r < rows_many ? s0 + u * 16 + r : rows_many - 1;
+            ps[u] = many + i * ld_many + group * 32;
+            es[u] = many_e + i * lde_many;
         }
 #pragma unroll
-        for (int h = 0; h < 4; ++h) {
-            bf16x8 wa[2], wb[2];
+        for (int t = 0; t < MT; ++t) {
+            const int64_t i = h0 + t * 16 + r < rows_few ? h0 + t * 16 + r : rows_few - 1;
+            ph[t] = few + i * ld_few + group * 32;
+            eh[t] = few_e + i * lde_few;
+        }
+        auto widen = [](const uint4 (&q)[2], float c, bf16x8 (&to)[4]) {
+            to[0] = widen8(q[0].x, q[0].y, c);
+            to[1] = widen8(q[0].z, q[0].w, c);
+            to[2] = widen8(q[1].x, q[1].y, c);
+            to[3] = widen8(q[1].z, q[1].w, c);
+        };
+        constexpr int kAhead = NT == 1 ? 4 : 2;                       // blocks of the many rows on their way at a time
+        uint4 qs[kAhead][NT][2];
+        uint8_t cs[kAhead][NT];
+        auto fetch = [&](int b, uint4 (&q)[NT][2], uint8_t (&c)[NT]) {
+            const int at = b < last ? b : last - 1;
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                wa[t] = (h & 1) ? widen8(fa[t][h / 2].z, fa[t][h / 2].w, ca[t]) : widen8(fa[t][h / 2].x, fa[t][h / 2].y, ca[t]);
-                wb[t] = (h & 1) ? widen8(fb[t][h / 2].z, fb[t][h / 2].w, cb[t]) : widen8(fb[t][h / 2].x, fb[t][h / 2].y, cb[t]);
+            for (int u = 0; u < NT; ++u) {
+                const uint4 *p = reinterpret_cast<const uint4 *>(ps[u] + (int64_t)at * 128);
+                q[u][0] = p[0];
+                q[u][1] = p[1];
+                c[u] = es[u][at];
             }
+        };
+        if (first < last) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int j = 0; j < kAhead; ++j) fetch(first + j, qs[j], cs[j]);
+            for (int b0 = first; b0 < last; b0 += kAhead) {
 #pragma unroll
-                for (int u = 0; u < 2; ++u) acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wa[t], wb[u], acc[t][u], 0, 0, 0);
+                for (int j = 0; j < kAhead; ++j) {
+                    const int b = b0 + j;
+                    if (b >= last) break;
+                    bf16x8 fs[NT][4];
+#pragma unroll
+                    for (int u = 0; u < NT; ++u) widen(qs[j][u], power_of(cs[j][u]), fs[u]);
+                    fetch(b + kAhead, qs[j], cs[j]);
+#pragma unroll
+                    for (int t = 0; t < MT; ++t) {
+                        const uint4 *p = reinterpret_cast<const uint4 *>(ph[t] + (int64_t)b * 128);
+                        const uint4 qh[2] = {p[0], p[1]};
+                        bf16x8 fh[4];
+                        widen(qh, power_of(eh[t][b]), fh);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+#pragma unroll
+                            for (int u = 0; u < NT; ++u) acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fs[u][k], fh[k], acc[t][u], 0, 0, 0);
+                    }
+                }
+            }
         }
     }
+    if (along > 1) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < MT; ++t)
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < NT; ++u) sums[wave][t * NT + u][lane] = acc[t][u];
+        __syncthreads();
+        if (mine != 0) return;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int64_t i = i0 + t * 16 + (lane >> 4) * 4 + q, j = j0 + u * 16 + r;
-                if (i < g.M && j < g.N) Elem<TO>::put(static_cast<TO *>(g.out) + i * g.ldo + j, acc[t][u][q]);
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int u = 0; u < NT; ++u)
+                for (int w = 1; w < along; ++w) acc[t][u] += sums[wave + w][t * NT + u][lane];
+    }
+    if (s0 >= rows_many) return;
+    TO *out = static_cast<TO *>(g.out);
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int u = 0; u < NT; ++u) {
+            const int64_t h = h0 + t * 16 + r, s = s0 + u * 16 + group * 4;
+            if (h >= rows_few || s >= rows_many) continue;
+            if (!turned && s + 4 <= rows_many) {
+                store4(out + h * g.ldo + s, acc[t][u]);
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (s + q < rows_many) Elem<TO>::put(out + (turned ? (s + q) * g.ldo + h : h * g.ldo + s + q), acc[t][u][q]);
             }
+        }
 }
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
@@ -148,9 +202,9 @@ struct Tile {
         const uint64_t at = (uint64_t)p;
         return i32x4{(int)(uint32_t)at, (int)(uint32_t)(at >> 32), 0x7FFFFFFF, 0x00020000};
     }
-    // ROWS: how many of A's rows of each wave row are fetched at a time
+    // ROWS: how many of A's rows of each wave row are fetched at a time; first: block at which the workgroup's sum begins, a multiple of four
     template <int ROWS>
-    __device__ void init(const MatmulArgs &g)
+    __device__ void init(const MatmulArgs &g, int first)
     {
         lane = threadIdx.x & 63;
         wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -160,8 +214,8 @@ struct Tile {
         j0 = (int64_t)tn * BN;
         left_m = (int)(g.M - i0 < BM ? g.M - i0 : BM);
         left_n = (int)(g.N - j0 < BN ? g.N - j0 : BN);
-        ra = resource(g.a + i0 * g.lda);
-        rb = resource(g.b + j0 * g.ldb);
+        ra = resource(g.a + i0 * g.lda + (int64_t)first * 128);
+        rb = resource(g.b + j0 * g.ldb + (int64_t)first * 128);
         const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
         constexpr int kUnit = 2 * ROWS, kUnits = BM / kUnit, kEach = LA / kUnits;      // rows of a unit, units, a wave's loads for one
 #pragma unroll
@@ -178,8 +232,8 @@ struct Tile {
             asm volatile("" : "+v"(from_b[t]));
         }
         // words of exponents: A's rows, then B's, 64 to an instruction, a wave's share in one or two
-        rea = resource(g.ea + i0 * g.lde_a);
-        reb = resource(g.eb + j0 * g.lde_b);
+        rea = resource(g.ea + i0 * g.lde_a + first);
+        reb = resource(g.eb + j0 * g.lde_b + first);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             const int c = exponent_chunk(t), r = (c < TM ? c : c - TM) * 64 + lane;
@@ -252,7 +306,7 @@ __device__ inline uint32_t lds_address(const void *p) { return (uint32_t)(size_t
 // Sums of fp32 accuracy (see the top).  A block is taken in four parts of 32: a wave holds B's part as bfloat16 and takes A's 32 rows in turn, a row
 // being TN x 2 instructions; the next row's codes are on their way and the one before them is widened meanwhile.  B's next part is widened as the last row's products release
 // its registers.  The barrier stands in front of the second to last row of a block: everything of it has been read, the next block is there, and the loads
-// of the one behind that leave, three to a row.
+// of the one behind that leave, a few to a row.
 template <int TM, int TN, typename TO>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM * TN > 8 ? 1 : 2, TM * TN > 8 ? 1 : 2))) void matmul_tile_kernel(MatmulArgs g)
 {
@@ -260,15 +314,19 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM * TN > 8
     constexpr int kStage = (G::BM + G::BN) * 128, kLoads = G::LA + G::LB;
     constexpr int kLds = 2 * kStage + 2 * G::kExps;
     static_assert(4 * 32 * 32 * TN * sizeof(TO) <= 2 * kStage, "room for the results");
-    static_assert(TM % 2 == 0 && 3 * 4 * TM >= kLoads + 6, "rows enough for the loads");
+    constexpr int kPer = TN < 3 ? TN : 3;                     // loads to a row
+    static_assert(TM % 2 == 0 && kPer * (4 * TM - 2) >= kLoads, "rows enough for the loads");
     __shared__ __attribute__((aligned(1024))) uint8_t lds[kLds];
     G tile;
-    tile.template init<G::BM / 2>(g);
+    // a part of the sum for each blockIdx.y, its results behind each other
+    const int first = blockIdx.y * g.each;
+    g.out = static_cast<TO *>(g.out) + (int64_t)blockIdx.y * g.M * g.N;
+    tile.template init<G::BM / 2>(g, first);
     const uint32_t lds0 = lds_address(lds);
     const int lane = tile.lane, wave = tile.wave;
     const int r = lane & 31, half = lane >> 5;
     const int row_a = (wave >> 1) * 32 * TM + r, row_b = G::BM + (wave & 1) * 32 * TN + r;
-    const int blocks = g.blocks, end = blocks - 1, groups_end = end >> 2;
+    const int blocks = g.blocks - first < g.each ? g.blocks - first : g.each, end = blocks - 1, groups_end = end >> 2;
 
     f32x16 acc[TM][TN];
 #pragma unroll
@@ -302,7 +360,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM * TN > 8
     for (int n = 0; n < kLoads; ++n) fetch(0, 0, n);
     asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" : : : "memory");
 #pragma unroll
-    for (int n = 0; n < 6; ++n) fetch(1, end < 1 ? end : 1, n);
+    for (int n = 0; n < 2 * kPer; ++n) fetch(1, end < 1 ? end : 1, n);
     tile.fetch_exponents(lds0 + 2 * kStage + G::kExps, 0, groups_end < 1 ? groups_end : 1);
     tile.fetch_exponents(lds0 + 2 * kStage + G::kExps, 1, groups_end < 1 ? groups_end : 1);
     qa[0] = read(row_a, 0, 0);
@@ -350,9 +408,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM * TN > 8
 #pragma unroll
                 for (int u = 0; u < TN; ++u) {
                     acc[t][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[u][0], fa[i & 1][0], acc[t][u], 0, 0, 0);
-                    // loads: three to a row, from the barrier on
-                    const int slot = ((i + 2) % (4 * TM)) * 3 + u;
-                    if (u < 3 && slot < kLoads) fetch(i >= 4 * TM - 2 ? b : b + 1, i >= 4 * TM - 2 ? ahead : later, slot);
+                    // loads from the barrier on
+                    const int slot = ((i + 2) % (4 * TM)) * kPer + u;
+                    if (u < kPer && slot < kLoads) fetch(i >= 4 * TM - 2 ? b : b + 1, i >= 4 * TM - 2 ? ahead : later, slot);
                     if (u == 0 && i == 4 * TM / 2) tile.fetch_exponents(lds0 + 2 * kStage + (((b >> 2) + 1) & 1) * G::kExps, b & 1, (b >> 2) < groups_end ? (b >> 2) + 1 : groups_end);
                     WPSGD_IN_ORDER;
                     acc[t][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[u][1], fa[i & 1][1], acc[t][u], 0, 0, 0);
@@ -380,7 +438,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     constexpr int kAtB = kUnits * kUnit, kAtE = kAtB + 2 * kB;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[kAtE + 2 * G::kExps];
     G tile;
-    tile.template init<64>(g);
+    tile.template init<64>(g, 0);
     const uint32_t lds0 = lds_address(lds);
     const int lane = tile.lane, wave = tile.wave;
     const int r = lane & 31, half = lane >> 5;
@@ -491,6 +549,77 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     tile.template store<uint16_t>(g, acc, lds + wave * (32 * 32 * TN * 2));
 }
 
+// The parts of a split sum, added in their order and rounded once.
+template <typename TO>
+__global__ __launch_bounds__(256) void join_parts_kernel(const float *parts, int count, int64_t M, int64_t N, TO *out, int64_t ldo)
+{
+    const int64_t all = M * N;
+    for (int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; at < all; at += (int64_t)gridDim.x * 1024) {
+        float s[4] = {0, 0, 0, 0};
+        const int n = (int)(all - at < 4 ? all - at : 4);
+        for (int p = 0; p < count; ++p) {
+            const float *from = parts + (int64_t)p * all + at;
+            if (n == 4) {
+                const Bytes16 q = load16(from);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[j] += __uint_as_float(q.w[j]);
+            } else {
+                for (int j = 0; j < n; ++j) s[j] += from[j];
+            }
+        }
+        const int64_t i = at / N, j = at - i * N;
+        if (n == 4 && j + 4 <= N) {
+            store4(out + i * ldo + j, f32x4{s[0], s[1], s[2], s[3]});
+        } else {
+            for (int q = 0; q < n; ++q) {
+                const int64_t ii = (at + q) / N, jj = at + q - ii * N;
+                Elem<TO>::put(out + ii * ldo + jj, s[q]);
+            }
+        }
+    }
+}
+
+// Which kernel, by sizes alone.
+struct MatmulPlan {
+    enum { Rows, Tile128, Tile256, Fast256 } kind;
+    int parts, each;           // Tile128: parts of the sum and blocks to each
+};
+static MatmulPlan plan_matmul(int64_t M, int64_t N, int64_t blocks, bool fast, bool wide_rows)
+{
+    const int64_t few = M < N ? M : N;
+    if (few <= 64 || wide_rows) return {MatmulPlan::Rows, 1, 0};
+    if (blocks == 0) return {MatmulPlan::Tile128, 0, 0};                      // a sum over nothing
+    const int64_t t256 = ((M + 255) / 256) * ((N + 255) / 256), t128 = ((M + 127) / 128) * ((N + 127) / 128);
+    if (t256 >= 192) return {fast ? MatmulPlan::Fast256 : MatmulPlan::Tile256, 1, (int)blocks};
+    int parts = 1;
+    while (t128 * parts < 256 && blocks >= parts * 16) parts *= 2;           // eight blocks to a part at least
+    const int each = (int)(((blocks + parts - 1) / parts + 3) / 4 * 4);
+    return {MatmulPlan::Tile128, each > 0 ? (int)((blocks + each - 1) / each) : 0, each};
+}
+template <int MT, int NT, typename TO>
+static hipError_t launch_rows_of(const MatmulArgs &g, bool turned, hipStream_t s)
+{
+    const int64_t many = turned ? g.M : g.N, few = turned ? g.N : g.M;
+    const int64_t groups = (many + 16 * NT - 1) / (16 * NT), panels = (few + 16 * MT - 1) / (16 * MT);
+    int along = 1;
+    while (along < kRowWaves && groups * panels * along < 2048 && g.blocks >= 2 * along) along *= 2;
+    const int64_t grid = (groups * along + kRowWaves - 1) / kRowWaves;
+    if (grid > 0x7FFFFFFFLL || panels > 65535) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((matmul_rows_kernel<MT, NT, TO>), dim3((unsigned)grid, (unsigned)panels), dim3(64 * kRowWaves), 0, s, g, along, turned);
+    return hipGetLastError();
+}
+template <typename TO>
+static hipError_t launch_rows(const MatmulArgs &g, hipStream_t s)
+{
+    const bool turned = g.M > g.N;
+    const int64_t many = turned ? g.M : g.N, few = turned ? g.N : g.M;
+    if (few <= 16) return many >= 32 * 2048 ? launch_rows_of<1, 2, TO>(g, turned, s) : launch_rows_of<1, 1, TO>(g, turned, s);
+    if (few <= 32) return many >= 32 * 2048 ? launch_rows_of<2, 2, TO>(g, turned, s) : launch_rows_of<2, 1, TO>(g, turned, s);
+    return many >= 32 * 2048 ? launch_rows_of<4, 2, TO>(g, turned, s) : launch_rows_of<4, 1, TO>(g, turned, s);
+}
+// rows of a tile are addressed with 32 bits
+static bool wide(int64_t ld, int64_t ld_exps) { return ld > (1LL << 22) || ld_exps > (1LL << 22); }
+
 }  // namespace wpsgd
 
 using namespace wpsgd;
@@ -499,8 +628,9 @@ extern "C" {
 
 size_t wpsgd_block_matmul_workspace(int64_t rows_a, int64_t rows_b, int64_t cols)
 {
-    (void)rows_a; (void)rows_b; (void)cols;
-    return 0;
+    if (rows_a <= 0 || rows_b <= 0 || cols <= 0) return 0;
+    const MatmulPlan p = plan_matmul(rows_a, rows_b, (cols + 127) / 128, false, false);
+    return p.parts > 1 ? ((size_t)p.parts * rows_a * rows_b * sizeof(float) + 255) & ~(size_t)255 : 0;
 }
 
 int wpsgd_block_matmul(const wpsgd_blocks *A, const wpsgd_blocks *B, void *out, int64_t ld_out, wpsgd_dtype dtype, void *workspace, size_t workspace_bytes,
@@ -515,21 +645,43 @@ int wpsgd_block_matmul(const wpsgd_blocks *A, const wpsgd_blocks *B, void *out, 
     const size_t need = wpsgd_block_matmul_workspace(A->rows, B->rows, A->cols);
     if (need && (!workspace || (uintptr_t)workspace % 256 != 0)) return WPSGD_INVALID_ARG;
     if (workspace_bytes < need) return WPSGD_WORKSPACE_TOO_SMALL;
-    const MatmulArgs g{static_cast<const uint8_t *>(A->codes), static_cast<const uint8_t *>(B->codes), static_cast<const uint8_t *>(A->exps),
-                       static_cast<const uint8_t *>(B->exps), A->ld, B->ld, A->ld_exps, B->ld_exps, A->rows, B->rows, (int)((A->cols + 127) / 128), out, ld_out};
-    const int64_t groups = ((A->rows + 63) / 64) * ((B->rows + 63) / 64);
-    if (groups > 0x7FFFFFFFLL) return WPSGD_UNSUPPORTED;
+    MatmulArgs g{static_cast<const uint8_t *>(A->codes), static_cast<const uint8_t *>(B->codes), static_cast<const uint8_t *>(A->exps),
+                 static_cast<const uint8_t *>(B->exps), A->ld, B->ld, A->ld_exps, B->ld_exps, A->rows, B->rows, (int)((A->cols + 127) / 128), out, ld_out, 0};
+    const bool f32 = dtype == WPSGD_F32;
+    const MatmulPlan p = plan_matmul(g.M, g.N, g.blocks, !f32, wide(g.lda, g.lde_a) || wide(g.ldb, g.lde_b));
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (A->rows >= 256 && B->rows >= 256 && g.blocks > 0) {
-        const dim3 grid((unsigned)(((B->rows + 255) / 256) * ((A->rows + 255) / 256)));
-        if (dtype == WPSGD_F32) hipLaunchKernelGGL((matmul_tile_kernel<4, 4, float>), grid, dim3(256), 0, s, g);
-        else hipLaunchKernelGGL(matmul_fast_kernel, grid, dim3(256), 0, s, g);
-        const hipError_t e = hipGetLastError();
-        return e == hipSuccess ? WPSGD_OK : hip_fail(e);
+    hipError_t e = hipSuccess;
+    if (p.kind == MatmulPlan::Rows) {
+        e = f32 ? launch_rows<float>(g, s) : launch_rows<uint16_t>(g, s);
+    } else {
+        const int64_t side = p.kind == MatmulPlan::Tile128 ? 128 : 256;
+        const int64_t tiles = ((g.M + side - 1) / side) * ((g.N + side - 1) / side);
+        if (tiles > 0x7FFFFFFFLL) return WPSGD_UNSUPPORTED;
+        g.each = p.each;
+        const dim3 grid((unsigned)tiles), block(256);
+        if (p.kind == MatmulPlan::Fast256) {
+            hipLaunchKernelGGL(matmul_fast_kernel, grid, block, 0, s, g);
+        } else if (p.kind == MatmulPlan::Tile256) {
+            hipLaunchKernelGGL((matmul_tile_kernel<4, 4, float>), grid, block, 0, s, g);
+        } else if (p.parts == 1) {
+            if (f32) hipLaunchKernelGGL((matmul_tile_kernel<2, 2, float>), grid, block, 0, s, g);
+            else hipLaunchKernelGGL((matmul_tile_kernel<2, 2, uint16_t>), grid, block, 0, s, g);
+        } else {
+            if (p.parts > 1) {
+                MatmulArgs part = g;
+                part.out = workspace;
+                part.ldo = g.N;
+                hipLaunchKernelGGL((matmul_tile_kernel<2, 2, float>), dim3((unsigned)tiles, (unsigned)p.parts), block, 0, s, part);
+                e = hipGetLastError();
+                if (e != hipSuccess) return hip_fail(e);
+            }
+            const int64_t quads = (g.M * g.N + 3) / 4, groups = (quads + 255) / 256;
+            const dim3 join((unsigned)(groups < 2048 ? groups : 2048));
+            if (f32) hipLaunchKernelGGL(join_parts_kernel<float>, join, block, 0, s, static_cast<const float *>(workspace), p.parts, g.M, g.N, static_cast<float *>(out), ld_out);
+            else hipLaunchKernelGGL(join_parts_kernel<uint16_t>, join, block, 0, s, static_cast<const float *>(workspace), p.parts, g.M, g.N, static_cast<uint16_t *>(out), ld_out);
+        }
+        e = hipGetLastError();
     }
-    if (dtype == WPSGD_F32) hipLaunchKernelGGL(matmul_simple_kernel<float>, dim3((unsigned)groups), dim3(256), 0, s, g);
-    else hipLaunchKernelGGL(matmul_simple_kernel<uint16_t>, dim3((unsigned)groups), dim3(256), 0, s, g);
-    const hipError_t e = hipGetLastError();
     return e == hipSuccess ? WPSGD_OK : hip_fail(e);
 }
 

@@ -520,6 +520,17 @@ def wpsgd_stream_rows(X: Matrix, groups, rows_per_group, seed=0, stream=None) ->
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
 
+def _stream_of(stream, t):
+    """The stream's handle; for None that of the current stream of t's device.  (These calls are short enough for the 2.6 us that
+    torch.cuda.current_stream takes to make an object of it to matter.)"""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(t.device.index)
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+_CODES = (torch.float8_e4m3fn, torch.uint8, torch.int8)
+
+
 @dataclass
 class BlockMatrix:
     """rows x cols in 8-bit floating point, a power of two for each block of 128 elements of a row:
@@ -531,22 +542,23 @@ class BlockMatrix:
     exps: torch.Tensor
 
     def c_struct(self) -> _CBlocks:
-        codes, exps = self.codes, self.exps
-        assert codes.is_cuda and exps.is_cuda and codes.element_size() == 1 and exps.dtype == torch.uint8
-        assert codes.dim() == 2 and exps.dim() == 2 and codes.shape[0] == self.rows and exps.shape[0] == self.rows
-        blocks = -(-self.cols // 128)
-        assert codes.shape[1] >= 128 * blocks and exps.shape[1] >= blocks
-        assert self.rows == 0 or self.cols == 0 or (codes.stride(1) == 1 and exps.stride(1) == 1)
-        return _CBlocks(self.rows, self.cols, codes.data_ptr(), codes.stride(0), exps.data_ptr(), exps.stride(0))
+        codes, exps, rows, cols = self.codes, self.exps, self.rows, self.cols
+        assert codes.is_cuda and exps.is_cuda and codes.dtype in _CODES and exps.dtype == torch.uint8
+        (r0, c0), (r1, c1), (ld, step), (ld_exps, step_exps) = codes.shape, exps.shape, codes.stride(), exps.stride()
+        assert r0 == r1 == rows and 128 * c1 >= cols and c0 >= (cols + 127) // 128 * 128
+        assert step == step_exps == 1 or rows == 0 or cols == 0
+        return _CBlocks(rows, cols, codes.data_ptr(), ld, exps.data_ptr(), ld_exps)
 
 
 def _call_workspace(workspace, need, device, stream):
-    """The caller's workspace, or a temporary one, as address and size."""
+    """The caller's workspace, or a temporary one, as address and size, and the tensor itself: whoever calls holds on to it until the
+    work is queued."""
     if workspace is None:
         if not need:
-            return None, 0
+            return None, 0, None
         workspace = _workspace(need, device, stream)
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        return workspace.data_ptr(), max(need, 256), workspace
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
 
 def wpsgd_quantize(X: Matrix, rows: Optional[torch.Tensor] = None, transpose=False, codes: Optional[torch.Tensor] = None,
@@ -554,21 +566,19 @@ def wpsgd_quantize(X: Matrix, rows: Optional[torch.Tensor] = None, transpose=Fal
     """Rows of a dense data set (all, or those that `rows`, int64 on the GPU, names) as a BlockMatrix, blocks along the
     columns; transpose=True: one row for each column of X, blocks along the rows taken."""
     cm = X.c_struct()
+    n, picked = X.m, None
     if rows is not None:
         assert rows.is_cuda and rows.dtype == torch.int64 and rows.is_contiguous()
-        n = rows.numel()
-    else:
-        n = X.m
+        n, picked = rows.numel(), rows.data_ptr()
     r, c = (X.d, n) if transpose else (n, X.d)
     blocks = -(-c // 128)
+    source = X.dense if X.dense is not None else X.vals
     if codes is None:
-        assert X.dense is not None
-        codes = torch.empty((r, 128 * blocks), dtype=torch.float8_e4m3fn, device=X.dense.device)
+        codes = torch.empty((r, 128 * blocks), dtype=torch.float8_e4m3fn, device=source.device)
     if exps is None:
-        exps = torch.empty((r, -(-blocks // 4) * 4), dtype=torch.uint8, device=codes.device)
+        exps = torch.empty((r, (blocks + 3) // 4 * 4), dtype=torch.uint8, device=source.device)
     out = BlockMatrix(r, c, codes, exps)
-    rc = load().wpsgd_quantize(ctypes.byref(cm), rows.data_ptr() if rows is not None else None, n, int(bool(transpose)),
-                               ctypes.byref(out.c_struct()), _stream(stream))
+    rc = load().wpsgd_quantize(ctypes.byref(cm), picked, n, 1 if transpose else 0, ctypes.byref(out.c_struct()), _stream_of(stream, source))
     if rc != OK:
         raise WpsgdError(rc, "wpsgd_quantize")
     return out
@@ -585,17 +595,19 @@ def wpsgd_block_matmul(A: BlockMatrix, B: BlockMatrix, out: Optional[torch.Tenso
         out = torch.empty((A.rows, B.rows), dtype=dtype, device=A.codes.device)
     assert out.is_cuda and out.dtype in _DTYPES and out.shape == (A.rows, B.rows) and (out.numel() == 0 or out.stride(1) == 1)
     L = load()
-    p, size = _call_workspace(workspace, L.wpsgd_block_matmul_workspace(A.rows, B.rows, A.cols), out.device, stream)
+    p, size, held = _call_workspace(workspace, L.wpsgd_block_matmul_workspace(A.rows, B.rows, A.cols), out.device, stream)
     rc = L.wpsgd_block_matmul(ctypes.byref(A.c_struct()), ctypes.byref(B.c_struct()), out.data_ptr(), max(out.stride(0), B.rows),
-                              _DTYPES[out.dtype], p, size, _stream(stream))
+                              _DTYPES[out.dtype], p, size, _stream_of(stream, out))
     if rc != OK:
         raise WpsgdError(rc, "wpsgd_block_matmul")
     return out
 
 
 def _rows_of(Z):
-    assert Z.is_cuda and Z.dim() == 2 and Z.dtype in _DTYPES and (Z.numel() == 0 or Z.stride(1) == 1)
-    return Z.shape[0], Z.shape[1], (Z.stride(0) if Z.shape[0] > 1 else max(Z.stride(0), Z.shape[1]))
+    n, c = Z.shape
+    ld, step = Z.stride()
+    assert Z.is_cuda and Z.dtype in _DTYPES and (step == 1 or n * c == 0)
+    return n, c, ld if n > 1 else max(ld, c)
 
 
 def wpsgd_softmax_loss_workspace(n, classes, dtype) -> int:
@@ -615,18 +627,18 @@ def wpsgd_softmax_loss(Z: torch.Tensor, labels: torch.Tensor, scale=1.0, row_wei
     assert loss.is_cuda and loss.dtype == torch.float32 and loss.is_contiguous() and loss.numel() == n
     if grad is True:
         grad = torch.empty((n, c), dtype=Z.dtype, device=Z.device)
-    g_ptr, g_ld = None, 0
-    if grad is not False and grad is not None:
+        g_ptr, g_ld = grad.data_ptr(), c
+    elif grad is not False and grad is not None:
         gn, gc, g_ld = _rows_of(grad)
-        assert grad.dtype == Z.dtype and (gn, gc) == (n, c)
+        assert grad.dtype == Z.dtype and gn == n and gc == c
         g_ptr = grad.data_ptr()
     else:
-        grad = None
+        grad, g_ptr, g_ld = None, None, 0
     L = load()
     dt = _DTYPES[Z.dtype]
-    p, size = _call_workspace(workspace, L.wpsgd_softmax_loss_workspace(n, c, dt), Z.device, stream)
+    p, size, held = _call_workspace(workspace, L.wpsgd_softmax_loss_workspace(n, c, dt), Z.device, stream)
     rc = L.wpsgd_softmax_loss(Z.data_ptr(), n, c, ld, dt, labels.data_ptr(), row_weights.data_ptr() if row_weights is not None else None,
-                              float(scale), loss.data_ptr(), g_ptr, g_ld, p, size, _stream(stream))
+                              float(scale), loss.data_ptr(), g_ptr, g_ld, p, size, _stream_of(stream, Z))
     if rc != OK:
         raise WpsgdError(rc, "wpsgd_softmax_loss")
     return loss, grad
@@ -672,8 +684,8 @@ def _norm_call(name, tensors, args, norm, workspace, stream):
         norm = torch.empty((), dtype=torch.float32, device=tensors.table.device)
     assert norm.is_cuda and norm.dtype == torch.float32 and norm.numel() == 1
     c_list = ctypes.byref(tensors.c_list)
-    p, size = _call_workspace(workspace, L.wpsgd_grad_norm_workspace(c_list), norm.device, stream)
-    rc = getattr(L, name)(c_list, *args, norm.data_ptr(), p, size, _stream(stream))
+    p, size, held = _call_workspace(workspace, L.wpsgd_grad_norm_workspace(c_list), norm.device, stream)
+    rc = getattr(L, name)(c_list, *args, norm.data_ptr(), p, size, _stream_of(stream, norm))
     if rc != OK:
         raise WpsgdError(rc, name)
     return norm
@@ -723,9 +735,9 @@ def wpsgd_draw_classes(Z: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=
     assert probs.is_cuda and probs.dtype == torch.float32 and probs.is_contiguous() and probs.numel() == n
     L = load()
     dt = _DTYPES[Z.dtype]
-    p, size = _call_workspace(workspace, L.wpsgd_draw_classes_workspace(n, c, dt), Z.device, stream)
+    p, size, held = _call_workspace(workspace, L.wpsgd_draw_classes_workspace(n, c, dt), Z.device, stream)
     rc = L.wpsgd_draw_classes(Z.data_ptr(), n, c, ld, dt, u.data_ptr(), ctypes.byref(rule), drawn.data_ptr(), probs.data_ptr(), p, size,
-                              _stream(stream))
+                              _stream_of(stream, Z))
     if rc != OK:
         raise WpsgdError(rc, "wpsgd_draw_classes")
     return drawn, probs

@@ -6,6 +6,7 @@
 // in, so neither does a draw, and a weight is off by 2^-32 of the largest at most.  The run's end is found digit by digit on the
 // scores' bits (four digits of eight bits, the counts or weights of each in LDS), and the draw walks the kept classes by index.
 #include <cmath>
+#include <type_traits>
 
 #include "class_ops.h"
 
@@ -36,33 +37,62 @@ __device__ inline uint32_t index_key(uint32_t i) { return (0xFFFFFFu - i) << 8; 
 __device__ inline uint32_t key_index(uint32_t k) { return 0xFFFFFFu - (k >> 8); }
 
 struct Weigh {
-    float top, slope, low;
-    // how many powers of two a weight is under the largest, negative or 0; -inf for no weight, and for every other score where the largest is +inf
-    __device__ float powers(float x) const { return x == top ? 0.0f : (x - top) * slope; }
-    __device__ uint32_t of_powers(float z) const
-    {
-        const float e = __builtin_amdgcn_exp2f(z);
-        return e >= low ? (uint32_t)fmaf(e, kOne, 0.5f) : 0u;           // (NaN: none)
-    }
+    float top, slope;
+    // powers of two that a weight is under the largest, negative or 0; top and slope are finite.  -inf and NaN have no weight.
+    __device__ float powers(float x) const { return (x - top) * slope; }
+    __device__ static uint32_t of_powers(float z) { return (uint32_t)fmaf(__builtin_amdgcn_exp2f(z), kOne, 0.5f); }
     __device__ uint32_t operator()(float x) const { return of_powers(powers(x)); }
 };
 
+// Sums over a wave and over the lanes up to each one, in whole numbers, on the DPP network.
+template <int CTRL, int ROW_MASK, typename U>
+__device__ inline U dpp_whole(U v)
+{
+    if constexpr (sizeof(U) == 4) return (U)dpp_move_bits<CTRL, ROW_MASK>((int)v);
+    else return (U)(uint32_t)dpp_move_bits<CTRL, ROW_MASK>((int)(uint32_t)(v >> 32)) << 32 | (uint32_t)dpp_move_bits<CTRL, ROW_MASK>((int)(uint32_t)v);
+}
+template <typename U>
+__device__ inline U up_to_lane(U v)                // with this lane's own
+{
+    v += dpp_whole<0x111, 0xF>(v);                 // row_shr 1, 2, 4, 8
+    v += dpp_whole<0x112, 0xF>(v);
+    v += dpp_whole<0x114, 0xF>(v);
+    v += dpp_whole<0x118, 0xF>(v);
+    v += dpp_whole<0x142, 0xA>(v);                 // lane 15 of a row to the next row: rows 1 and 3
+    v += dpp_whole<0x143, 0xC>(v);                 // lane 31 to rows 2 and 3
+    return v;
+}
+__device__ inline uint32_t of_lane(uint32_t v, int j) { return (uint32_t)__builtin_amdgcn_readlane((int)v, j); }
+__device__ inline uint64_t of_lane(uint64_t v, int j) { return (uint64_t)of_lane((uint32_t)(v >> 32), j) << 32 | of_lane((uint32_t)v, j); }
+template <typename U>
+__device__ inline U wave_total(U v) { return of_lane(up_to_lane(v), kWave - 1); }
+
 // ---- a row in a workgroup ----
-// Vector v of thread t holds classes (v NT + t) E and on, sixteen bytes: a wave's vectors are a run of 64 E classes, a "segment".  The row is read again for each
-// step, from the caches: kept in registers, its every element would stand in the code of every step.
-//   1. the largest score;
+// A wave owns a run of classes, in vectors of sixteen bytes to a lane; kRun vectors of a wave are a "segment".  The row is read again for each step, from the caches:
+// kept in registers, its every element would stand in the code of every step.
+//
+//   1. the largest score, which is what reads the row from memory;
 //   2. few classes kept (top_k <= NT): the top_k-th largest of the threads' own largest scores is a score that at least top_k classes reach; the classes that do
 //      go to a list in LDS (a few times top_k), and everything else is done there;
-//   3. else the end of the run: weights (or counts) in bins of 1/16 power of two below the largest, then the bin in which it lies as a list;
-//   4. the draw: the kept weight of every segment, the segment, the class.
-// Where a list has no room (scores that are nearly all alike) the digits are looked for among all classes of the row.
-constexpr int kBins = 1024, kCopies = 4;
+//   3. top_p: weights of a sample (each thread's largest, two vectors of each for the others) in bins of powers of two say between which bins the run ends, give
+//      or take kMargin top_p (1 - top_p) of the weight (a part's share of a whole is that much surer the nearer it is to none or all).  One pass over the row then adds up what lies above them by segments, lists what lies between, and has the weight of all: the
+//      run's end is looked for in the list, and its classes are added to their segments.  Where it is not in the list, or the list has no room, what has been added up
+//      corrects the sample for another try; after four the end is looked for among all classes digit by digit, and a pass adds up the segments;
+//   4. the draw: the segment in which the target lies, then the class.
+//
+// 256 rows of 131072 bfloat16 scores, a row to a compute unit: 14 us for the first step, which is bound by memory, 8 to 20 for a pass that forms weights
+// (17 instructions an element, four of them the power of two).
+constexpr int kBins = 1024, kCopies = 2;
 constexpr int kMostClasses = 1 << 18;
+
+constexpr int kShort = 256;
+constexpr double kMargin = 0.16;
 
 template <typename T, int NT, int CAP>
 struct Row {
     static constexpr int E = Elem<T>::kPer16, kWaves = NT / 64;
-    static constexpr int kSegments = kMostClasses / (64 * E);
+    static constexpr int kRun = 4;
+    static constexpr int kSegments = kMostClasses / (64 * E * kRun) + kWaves;
     static constexpr int kAtATime = 16 / E;        // vectors
     struct Shared {
         union {
@@ -70,29 +100,37 @@ struct Row {
             unsigned long long bins[kCopies][kBins];
         };
         uint64_t list[CAP];                        // key << 32 | class
-        union {
-            uint64_t segment[kSegments];
-            float tops[kWaves];
-        };
+        unsigned long long front[kShort];          // of the classes of a short list
+        uint32_t weight[kShort], place[kShort];
+        unsigned long long segment[kSegments];
+        float tops[2 * kWaves];
         uint32_t ties[kSegments];
         uint64_t found[2];
         uint64_t sums[kWaves];
         uint32_t count;
-        uint32_t cut;
     };
     Shared *sh;
     const T *z;
-    int c, t, vectors;                             // vectors: of a thread
+    int c, t, vectors;                             // vectors: of a lane
+    float scale;                                   // bins to a power of two
     Weigh weigh;
 
+    __device__ __forceinline__ int class_of(int v) const { return (((t >> 6) * vectors + v) * 64 + (t & 63)) * E; }
+    // which segment a class is in
+    __device__ __forceinline__ int segment_of(int i) const
+    {
+        const int vector = i / (64 * E), wave = vector / vectors;
+        return wave * runs() + (vector - wave * vectors) / kRun;
+    }
+    __device__ __forceinline__ int runs() const { return (vectors + kRun - 1) / kRun; }
     __device__ __forceinline__ Bytes16 fetch(int v) const
     {
-        const int64_t at = ((int64_t)v * NT + t) * E;
-        if (at + E <= c) return load16(z + at);
+        const int at = class_of(v);
+        if (v < vectors && at + E <= c) return load16(z + at);
         Bytes16 q;
 #pragma unroll
         for (int j = 0; j < 4; ++j) q.w[j] = E == 8 ? 0xFF80FF80u : 0xFF800000u;       // -inf
-        if (at < c) {
+        if (v < vectors && at < c) {
 #pragma unroll
             for (int j = 0; j < E - 1; ++j)
                 if (at + j < c) {
@@ -120,7 +158,7 @@ struct Row {
     {
         each_vector([&](int v, const Bytes16 &q) {
 #pragma unroll
-            for (int j = 0; j < E; ++j) f(Elem<T>::get(q.w, j), (v * NT + t) * E + j);
+            for (int j = 0; j < E; ++j) f(Elem<T>::get(q.w, j), class_of(v) + j);
         });
     }
     __device__ void barrier() const
@@ -129,7 +167,7 @@ struct Row {
     }
     __device__ __forceinline__ uint64_t group_sum(uint64_t v)
     {
-        for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
+        v = wave_total(v);
         barrier();
         if ((t & 63) == 0) sh->sums[t >> 6] = v;
         barrier();
@@ -139,20 +177,21 @@ struct Row {
         return s;
     }
     // Where in descending order of a 32-bit key the sum of the values reaches goal: the key, and the sum in front of it.  walk(f) calls f(key, value) for
-    // the classes of this thread that take part.  BITS: how many of the key's upper bits differ.
+    // the classes of this thread that take part, whose keys lie between lo and hi; digits that these share are not looked at.  BITS: how many of the key's upper bits may differ.
     template <int BITS, typename W>
-    __device__ __forceinline__ uint32_t select(W &&walk, uint64_t goal, uint64_t &before)
+    __device__ __forceinline__ uint32_t select(W &&walk, uint64_t goal, uint64_t &before, uint32_t lo = 0, uint32_t hi = 0xFFFFFFFFu)
     {
-        uint32_t prefix = 0;
+        const int differ = lo == hi ? 0 : 32 - __clz(lo ^ hi);           // lower bits that may differ
+        uint32_t prefix = differ >= 32 ? 0 : hi >> differ << differ;
         before = 0;
 #pragma unroll 1
-        for (int shift = 24; shift >= 32 - BITS; shift -= 8) {
+        for (int top = differ; top > 32 - BITS; top -= 8) {              // bits under `top` are not known yet
+            const int shift = top > 8 ? top - 8 : 0;
             barrier();
             for (int i = t; i < 256; i += NT) sh->hist[i] = 0;
             barrier();
-            const uint32_t want = shift < 24 ? prefix >> (shift + 8) : 0;
             walk([&](uint32_t key, uint64_t v) {
-                if ((shift == 24 || key >> (shift + 8) == want) && v) atomicAdd(reinterpret_cast<unsigned long long *>(&sh->hist[(key >> shift) & 255]), v);
+                if ((top == 32 || (key ^ prefix) >> top == 0) && v) atomicAdd(reinterpret_cast<unsigned long long *>(&sh->hist[(key >> shift) & (255u >> (8 - (top - shift)))]), v);
             });
             barrier();
             if (t < 64) {                          // four digits to a lane, the largest first
@@ -162,11 +201,7 @@ struct Row {
                     h[j] = sh->hist[255 - 4 * t - j];
                     mine += h[j];
                 }
-                uint64_t in = mine;
-                for (int d = 1; d < 64; d *= 2) {
-                    const uint64_t o = __shfl_up(in, d);
-                    if (t >= d) in += o;
-                }
+                const uint64_t in = up_to_lane(mine);
                 uint64_t front = before + in - mine;
                 if (front < goal && goal <= before + in) {
 #pragma unroll
@@ -183,24 +218,43 @@ struct Row {
             prefix |= (uint32_t)sh->found[0] << shift;
             before = sh->found[1];
         }
-        if (BITS == 16 && !(prefix >> 31)) prefix |= 0xFFFFu;         // (a negative bfloat16's key ends in ones)
+        if (BITS == 16) prefix = prefix >> 31 ? prefix & 0xFFFF0000u : prefix | 0xFFFFu;         // (a negative bfloat16's key ends in ones)
         return prefix;
     }
     static constexpr int kKeyBits = E == 8 ? 16 : 32;
-    __device__ __forceinline__ void add_to_list(float x, int i)
-    {
-        const uint32_t at = atomicAdd(&sh->count, 1u);
-        if (at < CAP) sh->list[at] = (uint64_t)key_of(x + 0.0f) << 32 | (uint32_t)i;
-    }
     template <typename F>
     __device__ __forceinline__ void each_listed(F &&f)
     {
         for (uint32_t i = t; i < sh->count; i += NT) f((uint32_t)(sh->list[i] >> 32), (uint32_t)sh->list[i]);
     }
-    // the bin of a score: how far it lies below the largest, in sixteenths of a power of two
-    __device__ static int bin_of_powers(float z)
+    // the least and the largest key in the list
+    __device__ __forceinline__ void list_range(uint32_t &lo, uint32_t &hi)
     {
-        const float d = z * -16.0f;
+        lo = 0xFFFFFFFFu;
+        hi = 0;
+        each_listed([&](uint32_t key, uint32_t) {
+            lo = key < lo ? key : lo;
+            hi = key > hi ? key : hi;
+        });
+        for (int d = 1; d < 64; d *= 2) {
+            const uint32_t a = __shfl_xor(lo, d), b = __shfl_xor(hi, d);
+            lo = a < lo ? a : lo;
+            hi = b > hi ? b : hi;
+        }
+        barrier();
+        if ((t & 63) == 0) sh->sums[t >> 6] = (uint64_t)hi << 32 | lo;
+        barrier();
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const uint32_t a = (uint32_t)sh->sums[w], b = (uint32_t)(sh->sums[w] >> 32);
+            lo = a < lo ? a : lo;
+            hi = b > hi ? b : hi;
+        }
+    }
+    // the bin of a score: how far it lies below the largest, in powers of two times scale
+    __device__ __forceinline__ int bin_of_powers(float z) const
+    {
+        const float d = z * -scale;
         return d < (float)(kBins - 1) ? (int)d : kBins - 1;
     }
     __device__ int bin_of(float x) const { return bin_of_powers(weigh.powers(x)); }
@@ -211,57 +265,84 @@ struct Row {
         if (t == 0) sh->count = 0;
         barrier();
     }
-    // the first bin at which the sum reaches goal and the sum in front of it, if all bins reach it; total: of all bins
-    __device__ __forceinline__ int find_bin(uint64_t goal, uint64_t &before)
+    // Adds up the copies of the bins and all bins in front of this thread's; returns the sum of all.
+    static constexpr int kMine = kBins / NT;       // bins of a thread
+    __device__ __forceinline__ uint64_t scan_bins(uint64_t (&front)[kMine + 1])
     {
-        constexpr int kEach = kBins / 64;
         barrier();
-        if (t < 64) {
-            uint64_t mine = 0;
+        uint64_t h[kMine], mine = 0;
 #pragma unroll
-            for (int j = 0; j < kEach; ++j) mine += sh->bins[0][t * kEach + j];
-            uint64_t in = mine;
-            for (int d = 1; d < 64; d *= 2) {
-                const uint64_t o = __shfl_up(in, d);
-                if (t >= d) in += o;
-            }
-            uint64_t front = in - mine;
-            if (front < goal && goal <= in) {
-                for (int j = 0; j < kEach; ++j) {
-                    const uint64_t h = sh->bins[0][t * kEach + j];
-                    if (front < goal && goal <= front + h) {
-                        sh->found[0] = (uint64_t)(t * kEach + j);
-                        sh->found[1] = front;
-                    }
-                    front += h;
-                }
-            }
+        for (int j = 0; j < kMine; ++j) {
+            h[j] = 0;
+#pragma unroll
+            for (int k = 0; k < kCopies; ++k) h[j] += sh->bins[k][t * kMine + j];
+            mine += h[j];
         }
+        const uint64_t in = up_to_lane(mine);
+        if ((t & 63) == 63) sh->sums[t >> 6] = in;
+        barrier();
+        uint64_t before = in - mine, all = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const uint64_t s = sh->sums[w];
+            before += w < (t >> 6) ? s : 0;
+            all += s;
+        }
+        front[0] = before;
+#pragma unroll
+        for (int j = 0; j < kMine; ++j) front[j + 1] = front[j] + h[j];
+        return all;
+    }
+    // the first bin at which the sum reaches goal (more than 0, at most the sum of all), and the sum in front of it
+    __device__ __forceinline__ int find_bin(const uint64_t (&front)[kMine + 1], uint64_t goal, uint64_t &before)
+    {
+        barrier();
+#pragma unroll
+        for (int j = 0; j < kMine; ++j)
+            if (front[j] < goal && goal <= front[j + 1]) {
+                sh->found[0] = (uint64_t)(t * kMine + j);
+                sh->found[1] = front[j];
+            }
         barrier();
         before = sh->found[1];
         return (int)sh->found[0];
     }
-    // sums of the bins' copies, into the first; returns the sum of all
-    __device__ __forceinline__ uint64_t merge_bins()
+    // Appends a lane's classes to the list: bit j of which for class i(j).  One addition to its length for the wave.
+    template <typename I>
+    __device__ __forceinline__ void append(uint32_t which, I &&i)
     {
-        barrier();
-        uint64_t mine = 0;
-        for (int i = t; i < kBins; i += NT) {
-            uint64_t s = sh->bins[0][i];
-#pragma unroll
-            for (int k = 1; k < kCopies; ++k) s += sh->bins[k][i];
-            sh->bins[0][i] = s;
-            mine += s;
+        const uint32_t n = (uint32_t)__popc(which), n_in = up_to_lane(n), all = of_lane(n_in, kWave - 1);
+        if (all == 0) return;
+        uint32_t at = 0;
+        if ((t & 63) == 0) at = atomicAdd(&sh->count, all);
+        at = of_lane(at, 0) + n_in - n;
+        while (which) {
+            const int j = __ffs(which) - 1;
+            which &= which - 1;
+            const int c = i(j);
+            if (at < CAP) sh->list[at] = (uint64_t)key_of(Elem<T>::load(z + c) + 0.0f) << 32 | (uint32_t)c;
+            ++at;
         }
-        return group_sum(mine);
     }
 };
+
+// The end of the run among all classes over `last`, by weight or by number.  Out of line: where it is needed thousands of scores are all but equal.
+template <typename T, int NT, int CAP>
+__device__ __attribute__((noinline)) uint32_t find_in_row(Row<T, NT, CAP> row, bool weights, float last, uint64_t goal, uint64_t &before)
+{
+    uint64_t b;
+    const uint32_t key = row.template select<Row<T, NT, CAP>::kKeyBits>(
+        [&](auto &&f) { row.each([&](float x, int) { if (x > last || (!weights && x == last)) f(key_of(x + 0.0f), weights ? (uint64_t)row.weigh(x) : 1ull); }); }, goal, b);
+    before = b;
+    return key;
+}
 
 template <typename T, int NT, int CAP>
 __global__ __launch_bounds__(NT) void draw_row_kernel(DrawArgs a)
 {
     using R = Row<T, NT, CAP>;
     constexpr int E = R::E;
+    constexpr float kInf = __builtin_inff();
     __shared__ typename R::Shared sh;
     R row;
     const int64_t at_row = blockIdx.x;
@@ -270,35 +351,41 @@ __global__ __launch_bounds__(NT) void draw_row_kernel(DrawArgs a)
     row.z = static_cast<const T *>(a.z) + at_row * a.ld;
     row.c = (int)a.c;
     row.t = t;
-    row.vectors = (int)((a.c + (int64_t)NT * E - 1) / ((int64_t)NT * E));
+    row.vectors = (int)((a.c + NT * E - 1) / (NT * E));
     const float temperature = a.rule.row_temperature ? a.rule.row_temperature[at_row] : a.rule.temperature;
     const int64_t top_k = a.rule.row_top_k ? a.rule.row_top_k[at_row] : a.rule.top_k;
     const float top_p = a.rule.row_top_p ? a.rule.row_top_p[at_row] : a.rule.top_p;
+    const float low = fminf(a.rule.row_min_p ? a.rule.row_min_p[at_row] : a.rule.min_p, 1.0f);   // (the largest always stays)
     const float u = a.u[at_row];
 
-    // the largest score, and each thread's own
-    float own = -__builtin_inff();
+    // the largest score, each thread's own, and the least of those
+    float own = -kInf;
     row.each([&](float x, int) { own = fmaxf(own, x); });
     {
-        const float m = wave_max(own);
-        if (lane == 0) sh.tops[wave] = m;
+        const float m = wave_max(own), n = -wave_max(own > -kInf ? -own : -kInf);
+        if (lane == 0) {
+            sh.tops[wave] = m;
+            sh.tops[R::kWaves + wave] = n;
+        }
     }
     __syncthreads();
-    float top = sh.tops[0];
+    float top = sh.tops[0], least = sh.tops[R::kWaves];
 #pragma unroll
-    for (int w = 1; w < NT / 64; ++w) top = fmaxf(top, sh.tops[w]);
+    for (int w = 1; w < NT / 64; ++w) {
+        top = fmaxf(top, sh.tops[w]);
+        least = fminf(least, sh.tops[R::kWaves + w]);
+    }
     __syncthreads();
     top += 0.0f;
-    const bool greedy = !(temperature > 0.0f);
-    float slope = kLog2eDraw / (greedy ? 1.0f : temperature);
     auto answer = [&](int64_t which, float p) {
         a.classes[at_row] = which;
         if (a.probs) a.probs[at_row] = p;
     };
-    if (top == -__builtin_inff()) {
+    if (top == -kInf) {
         if (t == 0) answer(-1, 0.0f);
         return;
     }
+    const bool greedy = !(temperature > 0.0f);
     if (greedy) {                                  // the lowest index of the largest score
         if (t == 0) sh.count = 0xFFFFFFFFu;
         __syncthreads();
@@ -311,214 +398,377 @@ __global__ __launch_bounds__(NT) void draw_row_kernel(DrawArgs a)
         if (t == 0) answer((int64_t)sh.count, 1.0f);
         return;
     }
+    const float slope = kLog2eDraw / temperature;
     row.weigh.top = top;
     row.weigh.slope = slope;
-    row.weigh.low = fminf(a.rule.row_min_p ? a.rule.row_min_p[at_row] : a.rule.min_p, 1.0f);     // (the largest always stays)
+    // A score can be worth a weight down to 32 powers of two below the largest; the threads' own span a part of the scores that matter: bins as fine as that allows.
+    const float span = (top - least) * slope;
+    row.scale = span < 8.0f ? fminf((float)kBins / (8.0f * span), 1e30f) : 16.0f;
     const Weigh weigh = row.weigh;
-
-    float floor = -__builtin_inff();               // what is kept: scores over it, and the first `ties` equal to it by index
-    uint64_t ties = 0, total = 0;
-    bool listed = false;                           // every kept class is in the list
-    auto walk_list = [&](auto &&value) { return [&, value](auto &&f) { row.each_listed([&](uint32_t key, uint32_t) { f(key, value(key)); }); }; };
-    auto walk_row = [&](auto &&value) { return [&, value](auto &&f) { row.each([&](float x, int) { if (x == x) f(key_of(x + 0.0f), value(x)); }); }; };
-    const bool cut_k = top_k > 0 && top_k < row.c;
-    if (cut_k && top_k <= NT) {
-        // a score that top_k of the threads' largest reach
-        row.clear_bins();
-        if (own > -__builtin_inff()) atomicAdd(&sh.bins[0][row.bin_of(own)], 1ull);
-        uint64_t front;
-        const uint64_t with = row.group_sum(own > -__builtin_inff() ? 1 : 0);
-        float reach = own;
-        if (with >= (uint64_t)top_k) {
-            const int bin = row.find_bin((uint64_t)top_k, front);
-            reach = own > -__builtin_inff() && row.bin_of(own) <= bin ? own : __builtin_inff();
-        }
-        reach = -wave_max(-reach);
-        __syncthreads();
-        if (lane == 0) sh.tops[wave] = reach;
-        __syncthreads();
-        reach = sh.tops[0];
-#pragma unroll
-        for (int w = 1; w < NT / 64; ++w) reach = fminf(reach, sh.tops[w]);
-        if (own >= reach) {
-            row.each_vector([&](int v, const Bytes16 &q) {
-                float most = Elem<T>::get(q.w, 0);
-#pragma unroll
-                for (int j = 1; j < E; ++j) most = fmaxf(most, Elem<T>::get(q.w, j));
-                if (most >= reach && most > -__builtin_inff()) {
-#pragma unroll
-                    for (int j = 0; j < E; ++j) {
-                        const float x = Elem<T>::get(q.w, j);
-                        if (x >= reach && x > -__builtin_inff()) row.add_to_list(x, (v * NT + t) * E + j);
-                    }
-                }
-            });
-        }
-        __syncthreads();
-        listed = sh.count <= CAP;
-    }
-    if (cut_k) {
-        uint64_t before = 0;
-        const auto one = [](auto) -> uint64_t { return 1; };
-        const uint64_t k = (uint64_t)top_k;
-        if (listed) {
-            if (sh.count > k) {
-                floor = of_key(row.template select<R::kKeyBits>(walk_list(one), k, before));
-                ties = k - before;
-            }
-        } else {
-            uint64_t some = 0;                     // classes that have a score at all
-            row.each([&](float x, int) { some += x > -__builtin_inff(); });
-            some = row.group_sum(some);
-            if (some > k) {
-                row.clear_bins();
-                row.each([&](float x, int) { if (x > -__builtin_inff()) atomicAdd(&sh.bins[lane % kCopies][row.bin_of(x)], 1ull); });
-                row.merge_bins();
-                const int bin = row.find_bin(k, before);
-                row.each([&](float x, int i) { if (x > -__builtin_inff() && row.bin_of(x) == bin) row.add_to_list(x, i); });
-                __syncthreads();
-                uint64_t in = 0;
-                if (sh.count <= CAP) {
-                    floor = of_key(row.template select<R::kKeyBits>(walk_list(one), k - before, in));
-                } else {
-                    before = 0;
-                    floor = of_key(row.template select<R::kKeyBits>(walk_row(one), k, in));
-                }
-                ties = k - before - in;
-            }
-        }
-    }
-    const uint64_t q_floor = floor > -__builtin_inff() ? weigh(floor) : 0;
-    if (listed) {
-        uint64_t mine = 0;
-        row.each_listed([&](uint32_t key, uint32_t) { mine += of_key(key) > floor ? weigh(of_key(key)) : 0; });
-        total = row.group_sum(mine) + ties * q_floor;
-    }
-    if (top_p < 1.0f) {
-        const float over = floor;
-        auto need_of = [&](uint64_t all) {
-            const double wanted = ceil((double)top_p * (double)all);
-            const uint64_t need = wanted > 1.0 ? (uint64_t)wanted : 1;
-            return need < all ? need : all;
-        };
-        uint64_t before = 0, need = 0;
-        float end = floor;
-        bool inside = true;                        // the run ends over the floor that top_k has set
-        if (listed) {
-            need = need_of(total);
-            inside = need <= total - ties * q_floor;
-            before = total - ties * q_floor;
-            if (inside)
-                end = of_key(row.template select<R::kKeyBits>(walk_list([&](uint32_t key) -> uint64_t { return of_key(key) > over ? weigh(of_key(key)) : 0; }), need, before));
-        } else {
-            row.clear_bins();
-            row.each([&](float x, int) {
-                const float z = weigh.powers(x);
-                const uint32_t q = weigh.of_powers(z);
-                if (x > over && q) atomicAdd(&sh.bins[lane % kCopies][row.bin_of_powers(z)], (unsigned long long)q);
-            });
-            const uint64_t sum = row.merge_bins();
-            need = need_of(sum + ties * q_floor);
-            inside = need <= sum;
-            before = sum;
-            if (inside) {
-                const int bin = row.find_bin(need, before);
-                row.each([&](float x, int i) { if (x > over && row.bin_of(x) == bin) row.add_to_list(x, i); });
-                __syncthreads();
-                uint64_t in = 0;
-                if (sh.count <= CAP) {
-                    end = of_key(row.template select<R::kKeyBits>(walk_list([&](uint32_t key) -> uint64_t { return weigh(of_key(key)); }), need - before, in));
-                } else {
-                    before = 0;
-                    end = of_key(row.template select<R::kKeyBits>(walk_row([&](float x) -> uint64_t { return x > over ? weigh(x) : 0; }), need, in));
-                }
-                before += in;
-            }
-        }
-        const uint64_t q = weigh(end);         // (the run ends at a class with weight)
-        ties = (need - before + q - 1) / q;
-        floor = end;
-        total = before + ties * q;
-    }
-    const uint64_t q_end = floor > -__builtin_inff() ? weigh(floor) : 0;
     auto target_of = [&](uint64_t all) {
         const uint64_t at = u > 0.0f ? (uint64_t)((double)u * (double)all) : 0;
         return at < all ? at : all - 1;
     };
-    if (listed) {
-        // by index: the ties that stay, then the class
-        const uint64_t target = target_of(total);
-        uint32_t last = 0xFFFFFFFFu;               // the highest index among the ties that stay
-        const uint32_t floor_key = key_of(floor + 0.0f);
-        uint64_t before;
+    auto need_of = [&](uint64_t all) {
+        const double wanted = ceil((double)top_p * (double)all);
+        const uint64_t need = wanted > 1.0 ? (uint64_t)wanted : 1;
+        return need < all ? need : all;
+    };
+    const auto one = [](auto) -> uint64_t { return 1; };
+    auto walk_list = [&](auto &&value) { return [&, value](auto &&f) { row.each_listed([&](uint32_t key, uint32_t) { f(key, value(key)); }); }; };
+
+    float floor = -kInf;                           // what is kept: scores over it, and the first `ties` equal to it by index
+    uint64_t ties = 0, total = 0;
+    bool listed = false;                           // every kept class is in the list
+    const bool cut_k = top_k > 0 && top_k < row.c;
+    // +inf, or a temperature so small that the slope is: the largest scores share everything
+    const bool sharp = !(top < kInf) || !(slope < kInf);
+    if (sharp) {
         uint64_t equal = 0;
-        row.each_listed([&](uint32_t key, uint32_t) { equal += key == floor_key; });
-        equal = row.group_sum(equal);
-        if (ties > 0 && equal > ties)
-            last = key_index(row.template select<24>([&](auto &&f) { row.each_listed([&](uint32_t key, uint32_t i) { f(index_key(i), key == floor_key ? 1ull : 0ull); }); }, ties, before));
-        const uint32_t which = key_index(row.template select<24>(
-            [&](auto &&f) {
-                row.each_listed([&](uint32_t key, uint32_t i) {
-                    const float x = of_key(key);
-                    f(index_key(i), x > floor || (key == floor_key && ties > 0 && i <= last) ? (uint64_t)weigh(x) : 0ull);
-                });
-            },
-            target + 1, before));
-        row.each_listed([&](uint32_t key, uint32_t i) {
-            if (i == which) answer((int64_t)i, (float)((double)weigh(of_key(key)) / (double)total));
-        });
-        return;
-    }
-    // the kept weight of each segment, and its ties
-    const bool tied = ties > 0;
-    __syncthreads();
-    row.each_vector([&](int v, const Bytes16 &q) {
-        uint64_t mine = 0;
-        uint32_t equal = 0;
+        row.each([&](float x, int) { equal += x == top; });
+        ties = row.group_sum(equal);
+        if (cut_k && (uint64_t)top_k < ties) ties = (uint64_t)top_k;
+        if (top_p < 1.0f) ties = (need_of(ties << 31) + (1ull << 31) - 1) >> 31;
+        floor = top;
+        total = ties << 31;
+    } else {
+        if (cut_k && top_k <= NT) {
+            // a score that top_k of the threads' largest reach
+            row.clear_bins();
+            const bool some = own > -kInf;
+            if (some) atomicAdd(&sh.bins[0][row.bin_of(own)], 1ull);
+            uint64_t fronts[R::kMine + 1];
+            const uint64_t with = row.scan_bins(fronts);
+            float reach = own;
+            if (with >= (uint64_t)top_k) {
+                uint64_t front;
+                const int bin = row.find_bin(fronts, (uint64_t)top_k, front);
+                reach = some && row.bin_of(own) <= bin ? own : kInf;
+            }
+            reach = -wave_max(-reach);
+            __syncthreads();
+            if (lane == 0) sh.tops[wave] = reach;
+            __syncthreads();
+            reach = sh.tops[0];
 #pragma unroll
-        for (int j = 0; j < E; ++j) {
-            const float x = Elem<T>::get(q.w, j);
-            const uint32_t w = weigh(x);
-            mine += x > floor ? w : 0u;
-            equal += tied && x == floor;
+            for (int w = 1; w < NT / 64; ++w) reach = fminf(reach, sh.tops[w]);
+            row.each_vector([&](int v, const Bytes16 &q) {
+                float most = Elem<T>::get(q.w, 0);
+#pragma unroll
+                for (int j = 1; j < E; ++j) most = fmaxf(most, Elem<T>::get(q.w, j));
+                if (__ballot(most >= reach && most > -kInf)) {
+                    uint32_t which = 0;
+#pragma unroll
+                    for (int j = 0; j < E; ++j) {
+                        const float x = Elem<T>::get(q.w, j);
+                        which |= x >= reach && x > -kInf ? 1u << j : 0u;
+                    }
+                    row.append(which, [&](int j) { return row.class_of(v) + j; });
+                }
+            });
+            __syncthreads();
+            listed = sh.count <= CAP;
         }
-        for (int d = 1; d < 64; d *= 2) mine += __shfl_xor(mine, d);
-        if (tied) {
-            for (int d = 1; d < 64; d *= 2) equal += __shfl_xor(equal, d);
+        if (listed && sh.count <= kShort) {
+            // A short list: each class is compared with each, NT / kShort threads to a class.  Its place in order and the weight in front of it say whether it is
+            // kept, the kept weight in front of it by index whether it is drawn.
+            constexpr int kParts = NT / kShort;
+            const int n = (int)sh.count, mine = t % kShort, part = t / kShort;
+            const uint64_t me = mine < n ? sh.list[mine] : 0;
+            const uint64_t order = me ^ 0xFFFFFFFFull;                   // larger: in front
+            if (t < kShort) {
+                const uint32_t q = t < n ? weigh(of_key((uint32_t)(me >> 32))) : 0u;
+                sh.weight[t] = q;
+                sh.place[t] = 0;
+                sh.front[t] = 0;
+            }
+            __syncthreads();
+            const uint32_t q = sh.weight[mine];
+            auto sum_in_front = [&](auto &&in_front) {                   // of the weights of those; how many
+                uint64_t w = 0;
+                uint32_t places = 0;
+#pragma unroll 4
+                for (int j = part; j < n; j += kParts) {
+                    const bool yes = in_front(sh.list[j]);
+                    w += yes ? sh.weight[j] : 0u;
+                    places += yes;
+                }
+                if (mine < n) {
+                    atomicAdd(&sh.front[mine], (unsigned long long)w);
+                    atomicAdd(&sh.place[mine], places);
+                }
+                __syncthreads();
+            };
+            sum_in_front([&](uint64_t o) { return (o ^ 0xFFFFFFFFull) > order; });
+            // the first top_k, those whose weight reaches min_p (a run from the front, too)
+            bool kept = mine < n && sh.place[mine] < (uint32_t)top_k && __builtin_amdgcn_exp2f(weigh.powers(of_key((uint32_t)(me >> 32)))) >= low;
+            const uint64_t all = row.group_sum(kept && part == 0 ? (uint64_t)q : 0);
+            const uint64_t front = sh.front[mine];
+            if (top_p < 1.0f) kept = kept && front < need_of(all);
+            total = top_p < 1.0f ? row.group_sum(kept && part == 0 ? (uint64_t)q : 0) : all;
+            __syncthreads();
+            if (t < kShort) {
+                sh.weight[t] = kept ? q : 0u;
+                sh.front[t] = 0;
+            }
+            __syncthreads();
+            sum_in_front([&](uint64_t o) { return (uint32_t)o < (uint32_t)me; });
+            const uint64_t target = target_of(total), before = sh.front[mine];
+            if (part == 0 && kept && before <= target && target < before + q) answer((int64_t)(uint32_t)me, (float)((double)q / (double)total));
+            return;
         }
-        if (lane == 0) {
-            sh.segment[v * (NT / 64) + wave] = mine;
-            sh.ties[v * (NT / 64) + wave] = equal;
+        if (cut_k) {
+            uint64_t before = 0;
+            const uint64_t k = (uint64_t)top_k;
+            uint32_t lo, hi;
+            if (listed) {
+                if (sh.count > k) {
+                    row.list_range(lo, hi);
+                    floor = of_key(row.template select<R::kKeyBits>(walk_list(one), k, before, lo, hi));
+                    ties = k - before;
+                }
+            } else {
+                uint64_t some = 0;                 // classes that have a score at all
+                row.each([&](float x, int) { some += x > -kInf; });
+                some = row.group_sum(some);
+                if (some > k) {
+                    row.clear_bins();
+                    row.each([&](float x, int) { if (x > -kInf) atomicAdd(&sh.bins[lane % kCopies][row.bin_of(x)], 1ull); });
+                    uint64_t fronts[R::kMine + 1];
+                    row.scan_bins(fronts);
+                    const int bin = row.find_bin(fronts, k, before);
+                    row.each_vector([&](int v, const Bytes16 &q) {
+                        uint32_t which = 0;
+#pragma unroll
+                        for (int j = 0; j < E; ++j) {
+                            const float x = Elem<T>::get(q.w, j);
+                            which |= x > -kInf && row.bin_of(x) == bin ? 1u << j : 0u;
+                        }
+                        row.append(which, [&](int j) { return row.class_of(v) + j; });
+                    });
+                    __syncthreads();
+                    uint64_t in = 0;
+                    if (sh.count <= CAP) {
+                        row.list_range(lo, hi);
+                        floor = of_key(row.template select<R::kKeyBits>(walk_list(one), k - before, in, lo, hi));
+                    } else {
+                        before = 0;
+                        floor = of_key(find_in_row(row, false, -kInf, k, in));
+                    }
+                    ties = k - before - in;
+                }
+            }
         }
-    });
+        if (low > 0.0f) {
+            // min_p: the least score whose weight reaches it, sixty-four tries at a time
+            uint32_t from = key_of(-kInf), to = key_of(top);             // reaches: not `from`, `to`
+            while (to - from > 1) {
+                const uint32_t step = (to - from + 63) / 64, at = from + step * (uint32_t)(lane + 1);
+                const bool reaches = at >= to || at < from || __builtin_amdgcn_exp2f(weigh.powers(of_key(at))) >= low;
+                const int first = __ffsll((unsigned long long)__ballot(reaches)) - 1;
+                const uint32_t hit = from + step * (uint32_t)(first + 1);
+                from = from + step * (uint32_t)first;
+                to = hit < to && hit > from ? hit : to;
+            }
+            if (key_of(floor) < from) {
+                floor = of_key(from);
+                ties = 0;
+            }
+        }
+        const uint64_t q_floor = ties > 0 ? weigh(floor) : 0;
+        if (listed) {
+            uint64_t mine = 0;
+            row.each_listed([&](uint32_t key, uint32_t) { mine += of_key(key) > floor ? weigh(of_key(key)) : 0; });
+            const uint64_t over = row.group_sum(mine);
+            total = over + ties * q_floor;
+            if (top_p < 1.0f) {
+                const uint64_t need = need_of(total);
+                uint64_t before = over;
+                const float last = floor;
+                if (need <= over) {
+                    uint32_t lo, hi;
+                    row.list_range(lo, hi);
+                    floor = of_key(row.template select<R::kKeyBits>(walk_list([&](uint32_t key) -> uint64_t { return of_key(key) > last ? weigh(of_key(key)) : 0; }), need, before, lo, hi));
+                }
+                const uint64_t q = weigh(floor);   // (the run ends at a class with weight)
+                ties = (need - before + q - 1) / q;
+                total = before + ties * q;
+            }
+            // by index: the ties that stay, then the class
+            const uint64_t target = target_of(total);
+            uint32_t last = 0xFFFFFFFFu;           // the highest index among the ties that stay
+            const uint32_t floor_key = key_of(floor + 0.0f);
+            uint64_t before, equal = 0;
+            row.each_listed([&](uint32_t key, uint32_t) { equal += key == floor_key; });
+            equal = row.group_sum(equal);
+            if (ties > 0 && equal > ties)
+                last = key_index(row.template select<24>([&](auto &&f) { row.each_listed([&](uint32_t key, uint32_t i) { f(index_key(i), key == floor_key ? 1ull : 0ull); }); }, ties, before, index_key((uint32_t)row.c - 1), index_key(0)));
+            const uint32_t which = key_index(row.template select<24>(
+                [&](auto &&f) {
+                    row.each_listed([&](uint32_t key, uint32_t i) {
+                        const float x = of_key(key);
+                        f(index_key(i), x > floor || (key == floor_key && ties > 0 && i <= last) ? (uint64_t)weigh(x) : 0ull);
+                    });
+                },
+                target + 1, before, index_key((uint32_t)row.c - 1), index_key(0)));
+            row.each_listed([&](uint32_t key, uint32_t i) {
+                if (i == which) answer((int64_t)i, (float)((double)weigh(of_key(key)) / (double)total));
+            });
+            return;
+        }
+    }
+
+    // The kept weight of each segment, and its ties.  BETWEEN: scores over the floor count where they are less than `sure` powers of two below the largest; down
+    // to `maybe` they go to the list, and the weight of all that do not count is returned (each thread's).
+    auto add_segments = [&](auto between, float sure, float maybe) -> uint64_t {
+        constexpr bool BETWEEN = decltype(between)::value;
+        const bool tied = !BETWEEN && ties > 0;
+        uint64_t rest = 0;
+        for (int g = 0; g < row.runs(); ++g) {
+            uint64_t mine = 0;
+            uint32_t equal = 0, listed_ones = 0;   // (bit v E + j)
+#pragma unroll 1
+            for (int h = 0; h < R::kRun; h += R::kAtATime) {
+                Bytes16 q[R::kAtATime];
+#pragma unroll
+                for (int v = 0; v < R::kAtATime; ++v) q[v] = row.fetch(g * R::kRun + h + v);
+#pragma unroll
+                for (int v = 0; v < R::kAtATime; ++v)
+#pragma unroll
+                    for (int j = 0; j < E; ++j) {
+                        const float x = Elem<T>::get(q[v].w, j);
+                        const float z = weigh.powers(x);
+                        const uint32_t w = x > floor ? weigh.of_powers(z) : 0u;
+                        if constexpr (BETWEEN) {
+                            const bool in = z > sure;
+                            mine += in ? w : 0u;
+                            rest += in ? 0u : w;
+                            listed_ones |= z > maybe && !in && x > floor ? 1u << (v * E + j) << (h * E) : 0u;
+                        } else {
+                            mine += w;
+                            equal += tied && x == floor;
+                        }
+                    }
+            }
+            if constexpr (BETWEEN) {
+                row.append(listed_ones, [&](int j) { return row.class_of(g * R::kRun + j / E) + j % E; });
+            }
+            mine = wave_total(mine);
+            if (tied) equal = wave_total(equal);
+            if (lane == 0) {
+                sh.segment[wave * row.runs() + g] = mine;
+                sh.ties[wave * row.runs() + g] = equal;
+            }
+        }
+        return rest;
+    };
+    const int segments = R::kWaves * row.runs();
+    bool added = false;
+    if (top_p < 1.0f && !sharp) {
+        row.clear_bins();
+        // each thread's largest as it is, and two vectors of each for all of its others
+        auto put = [&](float x, uint32_t times) {
+            const float z = weigh.powers(x);
+            const uint32_t w = x > floor ? weigh.of_powers(z) : 0u;
+            if (w) atomicAdd(&sh.bins[lane % kCopies][row.bin_of_powers(z)], (unsigned long long)w * times);
+        };
+        put(own, 2);
+        const int picks = row.vectors > 1 ? 2 : 1;
+        for (int i = 0; i < picks; ++i) {
+            const Bytes16 q = row.fetch((lane * 5 + wave + i * ((row.vectors + 1) / 2)) % row.vectors);
+#pragma unroll
+            for (int j = 0; j < E; ++j)
+                if (Elem<T>::get(q.w, j) < own) put(Elem<T>::get(q.w, j), (uint32_t)(2 * row.vectors / picks));
+        }
+        uint64_t fronts[R::kMine + 1];
+        const uint64_t sample = row.scan_bins(fronts), q_floor = ties > 0 ? weigh(floor) : 0;
+        double goal = (double)top_p * (double)sample, margin = kMargin * fmax((double)top_p * (1.0 - (double)top_p), 0.006) * (double)sample;     // in the sample's weight
+        uint64_t need = 0, over = 0, rest = 0, before = 0;
+        float end = floor;
+        bool found = false;
+        for (int tries = 0; tries < 4 && !found && sample > 0; ++tries) {
+            uint64_t sampled = 0;                  // the sample's weight over `sure`
+            float sure = 1.0f, maybe = -kInf;      // (even the largest may be the last)
+            __syncthreads();
+            if (goal - margin > 1.0) {
+                const double from = goal - margin < (double)sample ? goal - margin : (double)sample;
+                sure = (float)row.find_bin(fronts, (uint64_t)from, sampled) / -row.scale;
+            }
+            if (goal + margin < (double)sample) {
+                const int last = row.find_bin(fronts, (uint64_t)(goal + margin > 1.0 ? goal + margin : 1.0), before);
+                if (last < kBins - 1) maybe = (float)(last + 1) / -row.scale;
+            }
+            if (t == 0) sh.count = 0;
+            __syncthreads();
+            rest = row.group_sum(add_segments(std::true_type{}, sure, maybe));
+            uint64_t mine = 0;
+            for (int i = t; i < segments; i += NT) mine += sh.segment[i];
+            over = row.group_sum(mine);
+            need = need_of(over + rest + ties * q_floor);
+            if (need > over + rest) break;         // among the ties that top_k has left
+            mine = 0;
+            const bool room = sh.count <= CAP;
+            if (room) row.each_listed([&](uint32_t key, uint32_t) { mine += weigh(of_key(key)); });
+            const uint64_t list = row.group_sum(mine);
+            found = room && need > over && need <= over + list;
+            // what has been added up says what the sample's weights are worth on this side of `sure`
+            if (need > over) goal = (double)sampled + (double)(need - over) * ((double)(sample - sampled) / (double)rest);
+            else goal = (double)sampled * ((double)need / (double)over);
+            margin *= room ? 0.5 : 0.2;
+        }
+        uint32_t lo, hi;
+        if (found) {
+            row.list_range(lo, hi);
+            end = of_key(row.template select<R::kKeyBits>(walk_list([&](uint32_t key) -> uint64_t { return weigh(of_key(key)); }), need - over, before, lo, hi));
+            before += over;
+            const uint32_t end_key = key_of(end + 0.0f);
+            row.each_listed([&](uint32_t key, uint32_t i) {
+                if (key > end_key) atomicAdd(&sh.segment[row.segment_of((int)i)], (unsigned long long)weigh(of_key(key)));
+                else if (key == end_key) atomicAdd(&sh.ties[row.segment_of((int)i)], 1u);
+            });
+            added = true;
+        } else if (sample == 0 || need <= over + rest) {
+            const float last = floor;
+            if (sample == 0) {                     // nothing of the sample lies over the floor
+                uint64_t mine = 0;
+                row.each([&](float x, int) { mine += x > last ? weigh(x) : 0u; });
+                rest = row.group_sum(mine);
+                need = need_of(rest + ties * q_floor);
+            }
+            before = rest;
+            if (need <= over + rest) end = of_key(find_in_row(row, true, last, need, before));
+        } else {
+            before = over + rest;
+        }
+        const uint64_t q = weigh(end);             // (the run ends at a class with weight)
+        ties = (need - before + q - 1) / q;
+        floor = end;
+        total = before + ties * q;
+    }
+    if (!added) {
+        __syncthreads();
+        add_segments(std::false_type{}, 0.0f, 0.0f);
+    }
     __syncthreads();
-    // the first wave walks them: where the sum passes the target, with the ties that stay
-    const int segments = row.vectors * (NT / 64);
+    const bool tied = ties > 0;
+    const uint64_t q_end = sharp ? 1ull << 31 : tied ? weigh(floor) : 0;
+    // the first wave walks the segments: where the sum passes the target, with the ties that stay
     if (wave == 0) {
         if (!(top_p < 1.0f)) {
             uint64_t mine = 0;
             for (int i = lane; i < segments; i += 64) mine += sh.segment[i];
-            for (int d = 1; d < 64; d *= 2) mine += __shfl_xor(mine, d);
-            total = mine + ties * q_end;
+            total = wave_total(mine) + ties * q_end;
         }
         const uint64_t target = target_of(total);
         uint64_t seen = 0, used = 0;               // in front of these 64 segments
         for (int base = 0; base < segments; base += 64) {
             const int i = base + lane;
             uint64_t w = i < segments ? sh.segment[i] : 0, n = i < segments && tied ? sh.ties[i] : 0;
-            uint64_t n_in = n;
-            for (int d = 1; d < 64; d *= 2) {
-                const uint64_t o = __shfl_up(n_in, d);
-                if (lane >= d) n_in += o;
-            }
+            const uint64_t n_in = up_to_lane(n);
             const uint64_t n_front = used + n_in - n;
             const uint64_t stay = n_front < ties ? (ties - n_front < n ? ties - n_front : n) : 0;
             w += stay * q_end;
-            uint64_t w_in = w;
-            for (int d = 1; d < 64; d *= 2) {
-                const uint64_t o = __shfl_up(w_in, d);
-                if (lane >= d) w_in += o;
-            }
+            const uint64_t w_in = up_to_lane(w);
             const uint64_t front = seen + w_in - w;
             if (front <= target && target < front + w) {
                 sh.found[0] = target - front;
@@ -526,48 +776,45 @@ __global__ __launch_bounds__(NT) void draw_row_kernel(DrawArgs a)
                 sh.count = (uint32_t)i;
                 sh.sums[0] = total;
             }
-            seen = __shfl(seen + w_in, 63);
-            used = __shfl(used + n_in, 63);
+            seen += of_lane(w_in, 63);
+            used += of_lane(n_in, 63);
             if (seen > target) break;
         }
     }
     __syncthreads();
     const int segment = (int)sh.count;
-    if (segment % (NT / 64) != wave) return;
+    if (segment / row.runs() != wave) return;
     total = sh.sums[0];
-    const uint64_t inside = sh.found[0], front_ties = sh.found[1];
-    const Bytes16 q = row.fetch(segment / (NT / 64));
-    uint32_t w[E], equal = 0;
-    uint64_t mine = 0;
+    uint64_t inside = sh.found[0], rank0 = sh.found[1];
+    for (int v = (segment % row.runs()) * R::kRun; v < (segment % row.runs() + 1) * R::kRun; ++v) {
+        const Bytes16 q = row.fetch(v);
+        uint32_t w[E], equal = 0;
+        uint64_t mine = 0;
 #pragma unroll
-    for (int j = 0; j < E; ++j) equal += tied && Elem<T>::get(q.w, j) == floor;
-    uint32_t n_in = equal;
-    for (int d = 1; d < 64; d *= 2) {
-        const uint32_t o = __shfl_up(n_in, d);
-        if (lane >= d) n_in += o;
-    }
-    uint64_t rank = front_ties + n_in - equal;
-#pragma unroll
-    for (int j = 0; j < E; ++j) {
-        const float x = Elem<T>::get(q.w, j);
-        const bool tie = tied && x == floor;
-        w[j] = x > floor || (tie && rank < ties) ? weigh(x) : 0u;
-        rank += tie;
-        mine += w[j];
-    }
-    uint64_t in = mine;
-    for (int d = 1; d < 64; d *= 2) {
-        const uint64_t o = __shfl_up(in, d);
-        if (lane >= d) in += o;
-    }
-    uint64_t front = in - mine;
-    if (front <= inside && inside < in) {
+        for (int j = 0; j < E; ++j) equal += tied && Elem<T>::get(q.w, j) == floor;
+        const uint32_t n_in = up_to_lane(equal);
+        uint64_t rank = rank0 + n_in - equal;
 #pragma unroll
         for (int j = 0; j < E; ++j) {
-            if (front <= inside && inside < front + w[j])
-                answer(((int64_t)(segment / (NT / 64)) * NT + t) * E + j, (float)((double)w[j] / (double)total));
-            front += w[j];
+            const float x = Elem<T>::get(q.w, j);
+            const bool tie = tied && x == floor;
+            w[j] = tie ? (rank < ties ? (uint32_t)q_end : 0u) : x > floor ? weigh(x) : 0u;
+            rank += tie;
+            mine += w[j];
         }
+        const uint64_t in = up_to_lane(mine);
+        uint64_t front = in - mine;
+        if (front <= inside && inside < in) {
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                if (front <= inside && inside < front + w[j]) answer((int64_t)row.class_of(v) + j, (float)((double)w[j] / (double)total));
+                front += w[j];
+            }
+        }
+        const uint64_t all = of_lane(in, 63);
+        if (inside < all) return;
+        inside -= all;
+        rank0 += of_lane(n_in, 63);
     }
 }
 
@@ -577,7 +824,7 @@ static hipError_t launch_draw(const DrawArgs &a, hipStream_t s)
     const dim3 grid((unsigned)a.n);
     // short rows: four waves, several workgroups to a compute unit
     if (a.c <= 4096) hipLaunchKernelGGL((draw_row_kernel<T, 256, 2048>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((draw_row_kernel<T, 1024, 8192>), grid, dim3(1024), 0, s, a);
+    else hipLaunchKernelGGL((draw_row_kernel<T, 1024, 14336>), grid, dim3(1024), 0, s, a);
     return hipGetLastError();
 }
 

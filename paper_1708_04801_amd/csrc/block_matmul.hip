@@ -46,14 +46,21 @@ __device__ inline void store4(uint16_t *p, const f32x4 &v)
 }
 
 // Few rows against many.  The one operand's rows (the class vectors of a serving call) are read once, straight from memory into the matrix instructions, sixteen
-// rows times NT to a wave; the other's 16 MT rows come from the caches with every block.  kWaves waves to a workgroup: `along` of them share the blocks of the
-// sum and add up through LDS, in their order, the others take the next rows.  Bound by memory: 16 x 65536 x 4096 reads 268 MB.
+// rows times NT to a wave; the other's 16 MT rows lie in LDS as bfloat16 fragments, a few blocks of the sum at a time (asked for by each wave
+// they are a trip to the L2 a block: 16 x 65536 x 4096 79 us, 64 x 65536 x 4096 138).  kRowWaves waves to a workgroup: `along` of them share the blocks of the
+// sum in turn and add up through LDS, in their order, the others take the next rows.  Bound by memory: 16 x 65536 x 4096 reads 268 MB.
 // `turned`: the many rows are A's (results of a lane lie below each other), else B's (beside each other).
 constexpr int kRowWaves = 8;
+constexpr int kHeldBlocks = 16;                                       // of sixteen rows: 64 KiB
 template <int MT, int NT, typename TO>
 __global__ __launch_bounds__(64 * kRowWaves) void matmul_rows_kernel(MatmulArgs g, int along, bool turned)
 {
-    __shared__ f32x4 sums[kRowWaves][MT * NT][64];
+    constexpr int kHeld = kHeldBlocks / MT;
+    constexpr int kAhead = 2;                                         // blocks of the many rows on their way at a time (four: 64 us instead of 57)
+    __shared__ union {
+        bf16x8 held[kHeldBlocks * 4][64];                             // block, rows, quarter: a fragment for each lane
+        f32x4 sums[kRowWaves][MT * NT][64];
+    } lds;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint8_t *many = turned ? g.a : g.b, *few = turned ? g.b : g.a, *many_e = turned ? g.ea : g.eb, *few_e = turned ? g.eb : g.ea;
     const int64_t ld_many = turned ? g.lda : g.ldb, ld_few = turned ? g.ldb : g.lda, lde_many = turned ? g.lde_a : g.lde_b, lde_few = turned ? g.lde_b : g.lde_a;
@@ -61,87 +68,94 @@ __global__ __launch_bounds__(64 * kRowWaves) void matmul_rows_kernel(MatmulArgs 
     const int across = kRowWaves / along, mine = wave % along;
     const int64_t s0 = ((int64_t)blockIdx.x * across + wave / along) * (16 * NT), h0 = (int64_t)blockIdx.y * (16 * MT);
     const int r = lane & 15, group = lane >> 4;
-    const int each = (g.blocks + along - 1) / along;
-    const int first = mine * each, last = first + each < g.blocks ? first + each : g.blocks;
+    const bool idle = s0 >= rows_many;
     f32x4 acc[MT][NT];
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
         for (int u = 0; u < NT; ++u) acc[t][u] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    if (s0 < rows_many) {
-        const uint8_t *ps[NT], *es[NT], *ph[MT], *eh[MT];
+    const uint8_t *ps[NT], *es[NT];
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+        const int64_t i = s0 + u * 16 + r < rows_many ? s0 + u * 16 + r : rows_many - 1;
+        ps[u] = many + i * ld_many + group * 16;                      // (an instruction takes 64 bytes of a row)
+        es[u] = many_e + i * lde_many;
+    }
+    uint4 qs[kAhead][NT][2];
+    uint8_t cs[kAhead][NT];
+    auto fetch = [&](int step, int j) {
+        const int b = step * along + mine, at = b < g.blocks ? b : g.blocks - 1;
 #pragma unroll
         for (int u = 0; u < NT; ++u) {
-            const int64_t i = s0 + u * 16 + r < rows_many ? s0 + u * 16 + r : rows_many - 1;
-            ps[u] = many + i * ld_many + group * 32;
-            es[u] = many_e + i * lde_many;
+            const uint4 *p = reinterpret_cast<const uint4 *>(ps[u] + (int64_t)at * 128);
+            qs[j][u][0] = p[0];
+            qs[j][u][1] = p[4];
+            cs[j][u] = es[u][at];
         }
+    };
+    const int per = kHeld / along;                                    // steps of a wave between two fillings
+    const int steps = (g.blocks + kHeld - 1) / kHeld * per;           // the same for every wave
+    if (steps > 0) {
 #pragma unroll
-        for (int t = 0; t < MT; ++t) {
-            const int64_t i = h0 + t * 16 + r < rows_few ? h0 + t * 16 + r : rows_few - 1;
-            ph[t] = few + i * ld_few + group * 32;
-            eh[t] = few_e + i * lde_few;
-        }
-        auto widen = [](const uint4 (&q)[2], float c, bf16x8 (&to)[4]) {
-            to[0] = widen8(q[0].x, q[0].y, c);
-            to[1] = widen8(q[0].z, q[0].w, c);
-            to[2] = widen8(q[1].x, q[1].y, c);
-            to[3] = widen8(q[1].z, q[1].w, c);
-        };
-        constexpr int kAhead = NT == 1 ? 4 : 2;                       // blocks of the many rows on their way at a time
-        uint4 qs[kAhead][NT][2];
-        uint8_t cs[kAhead][NT];
-        auto fetch = [&](int b, uint4 (&q)[NT][2], uint8_t (&c)[NT]) {
-            const int at = b < last ? b : last - 1;
+        for (int j = 0; j < kAhead; ++j) fetch(j, j);
+    }
+    for (int step0 = 0; step0 < steps; step0 += kAhead) {
 #pragma unroll
-            for (int u = 0; u < NT; ++u) {
-                const uint4 *p = reinterpret_cast<const uint4 *>(ps[u] + (int64_t)at * 128);
-                q[u][0] = p[0];
-                q[u][1] = p[1];
-                c[u] = es[u][at];
-            }
-        };
-        if (first < last) {
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j) fetch(first + j, qs[j], cs[j]);
-            for (int b0 = first; b0 < last; b0 += kAhead) {
-#pragma unroll
-                for (int j = 0; j < kAhead; ++j) {
-                    const int b = b0 + j;
-                    if (b >= last) break;
-                    bf16x8 fs[NT][4];
-#pragma unroll
-                    for (int u = 0; u < NT; ++u) widen(qs[j][u], power_of(cs[j][u]), fs[u]);
-                    fetch(b + kAhead, qs[j], cs[j]);
-#pragma unroll
-                    for (int t = 0; t < MT; ++t) {
-                        const uint4 *p = reinterpret_cast<const uint4 *>(ph[t] + (int64_t)b * 128);
-                        const uint4 qh[2] = {p[0], p[1]};
-                        bf16x8 fh[4];
-                        widen(qh, power_of(eh[t][b]), fh);
-#pragma unroll
-                        for (int k = 0; k < 4; ++k)
-#pragma unroll
-                            for (int u = 0; u < NT; ++u) acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fs[u][k], fh[k], acc[t][u], 0, 0, 0);
-                    }
+        for (int j = 0; j < kAhead; ++j) {
+            const int step = step0 + j;
+            if (step >= steps) break;
+            if (step % per == 0) {
+                const int b0 = step / per * kHeld, n = g.blocks - b0 < kHeld ? g.blocks - b0 : kHeld;
+                if (step > 0) __syncthreads();
+                for (int item = wave; item < n * MT * 2; item += kRowWaves) {      // block, rows, half
+                    const int h = item & 1, t = (item >> 1) % MT, b = b0 + (item >> 1) / MT;
+                    const int64_t i = h0 + t * 16 + r < rows_few ? h0 + t * 16 + r : rows_few - 1;
+                    const uint4 q = *reinterpret_cast<const uint4 *>(few + i * ld_few + (int64_t)b * 128 + h * 64 + group * 16);
+                    const float c = power_of(few_e[i * lde_few + b]);
+                    lds.held[(item >> 1) * 4 + h * 2][lane] = widen8(q.x, q.y, c);
+                    lds.held[(item >> 1) * 4 + h * 2 + 1][lane] = widen8(q.z, q.w, c);
                 }
+                __syncthreads();
             }
+            const int b = step * along + mine;
+            if (b < g.blocks && !idle) {
+                bf16x8 fs[NT][4];
+#pragma unroll
+                for (int u = 0; u < NT; ++u) {
+                    const float c = power_of(cs[j][u]);
+                    fs[u][0] = widen8(qs[j][u][0].x, qs[j][u][0].y, c);
+                    fs[u][1] = widen8(qs[j][u][0].z, qs[j][u][0].w, c);
+                    fs[u][2] = widen8(qs[j][u][1].x, qs[j][u][1].y, c);
+                    fs[u][3] = widen8(qs[j][u][1].z, qs[j][u][1].w, c);
+                }
+                const int at = b % kHeld;
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const bf16x8 fh = lds.held[(at * MT + t) * 4 + k][lane];
+#pragma unroll
+                        for (int u = 0; u < NT; ++u) acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fs[u][k], fh, acc[t][u], 0, 0, 0);
+                    }
+            }
+            fetch(step + kAhead, j);
         }
     }
     if (along > 1) {
+        __syncthreads();
 #pragma unroll
         for (int t = 0; t < MT; ++t)
 #pragma unroll
-            for (int u = 0; u < NT; ++u) sums[wave][t * NT + u][lane] = acc[t][u];
+            for (int u = 0; u < NT; ++u) lds.sums[wave][t * NT + u][lane] = acc[t][u];
         __syncthreads();
         if (mine != 0) return;
 #pragma unroll
         for (int t = 0; t < MT; ++t)
 #pragma unroll
             for (int u = 0; u < NT; ++u)
-                for (int w = 1; w < along; ++w) acc[t][u] += sums[wave + w][t * NT + u][lane];
+                for (int w = 1; w < along; ++w) acc[t][u] += lds.sums[wave + w][t * NT + u][lane];
     }
-    if (s0 >= rows_many) return;
+    if (idle) return;
     TO *out = static_cast<TO *>(g.out);
 #pragma unroll
     for (int t = 0; t < MT; ++t)
@@ -579,30 +593,40 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const float *parts, int
     }
 }
 
-// Which kernel, by sizes alone.
+// Which kernel, by sizes and the results' type alone.  Few rows: the one that reads the others once.  Else the one that should take the least time (us, measured for 1024 x 1024
+// to 16384 x 4096 results and 4 to 64 blocks of the sum): a round of tiles on all compute units takes 0.98 a block for 128 x 128 (two workgroups to a unit, so that
+// one's products hide the other's loads and results), 2.2 for 256 x 256 with fp32 sums and 1.09 in the 8-bit instruction (one to a unit, results not
+// hidden).  4096 x 4096, 8 blocks: fp32 41 | 38 (128 | 256), bfloat16 43 | 26; 5003 x 3001, 8 blocks, fp32: 38 | 42; 2048 x 2048, 64 blocks: 64 | 80 (8-bit).
 struct MatmulPlan {
     enum { Rows, Tile128, Tile256, Fast256 } kind;
     int parts, each;           // Tile128: parts of the sum and blocks to each
 };
-static MatmulPlan plan_matmul(int64_t M, int64_t N, int64_t blocks, bool fast, bool wide_rows)
+static MatmulPlan plan_matmul(int64_t M, int64_t N, int64_t blocks, bool f32, bool wide_rows)
 {
     const int64_t few = M < N ? M : N;
     if (few <= 64 || wide_rows) return {MatmulPlan::Rows, 1, 0};
     if (blocks == 0) return {MatmulPlan::Tile128, 0, 0};                      // a sum over nothing
     const int64_t t256 = ((M + 255) / 256) * ((N + 255) / 256), t128 = ((M + 127) / 128) * ((N + 127) / 128);
-    if (t256 >= 192) return {fast ? MatmulPlan::Fast256 : MatmulPlan::Tile256, 1, (int)blocks};
     int parts = 1;
     while (t128 * parts < 256 && blocks >= parts * 16) parts *= 2;           // eight blocks to a part at least
-    const int each = (int)(((blocks + parts - 1) / parts + 3) / 4 * 4);
-    return {MatmulPlan::Tile128, each > 0 ? (int)((blocks + each - 1) / each) : 0, each};
+    const int each = parts == 1 ? (int)blocks : (int)(((blocks + parts - 1) / parts + 3) / 4 * 4);
+    parts = (int)((blocks + each - 1) / each);
+    const double out = (double)M * (double)N * (f32 ? 4.0 : 2.0) / 4.6e6;    // to write the results
+    const auto rounds = [](int64_t tiles) { return tiles < 256 ? 1.0 : (double)tiles / 256.0; };
+    const double by128 = 5.0 + 0.98 * each * rounds(t128 * parts) + 0.5 * out + (parts > 1 ? 4.0 : 0.0);
+    const double by256 = (f32 ? 13.0 + 2.2 * (double)blocks * rounds(t256) : 10.0 + 1.09 * (double)blocks * rounds(t256)) + out;
+    if (by256 < by128) return {f32 ? MatmulPlan::Tile256 : MatmulPlan::Fast256, 1, (int)blocks};
+    return {MatmulPlan::Tile128, parts, each};
 }
+static size_t parts_bytes(const MatmulPlan &p, int64_t M, int64_t N) { return p.parts > 1 ? ((size_t)p.parts * M * N * sizeof(float) + 255) & ~(size_t)255 : 0; }
+
 template <int MT, int NT, typename TO>
 static hipError_t launch_rows_of(const MatmulArgs &g, bool turned, hipStream_t s)
 {
     const int64_t many = turned ? g.M : g.N, few = turned ? g.N : g.M;
     const int64_t groups = (many + 16 * NT - 1) / (16 * NT), panels = (few + 16 * MT - 1) / (16 * MT);
     int along = 1;
-    while (along < kRowWaves && groups * panels * along < 2048 && g.blocks >= 2 * along) along *= 2;
+    while (along < kRowWaves && along < kHeldBlocks / MT && groups * panels * along < 2048 && g.blocks >= 2 * along) along *= 2;
     const int64_t grid = (groups * along + kRowWaves - 1) / kRowWaves;
     if (grid > 0x7FFFFFFFLL || panels > 65535) return hipErrorInvalidValue;
     hipLaunchKernelGGL((matmul_rows_kernel<MT, NT, TO>), dim3((unsigned)grid, (unsigned)panels), dim3(64 * kRowWaves), 0, s, g, along, turned);
@@ -613,7 +637,8 @@ static hipError_t launch_rows(const MatmulArgs &g, hipStream_t s)
 {
     const bool turned = g.M > g.N;
     const int64_t many = turned ? g.M : g.N, few = turned ? g.N : g.M;
-    if (few <= 16) return many >= 32 * 2048 ? launch_rows_of<1, 2, TO>(g, turned, s) : launch_rows_of<1, 1, TO>(g, turned, s);
+    // too few rows for the compute units: the few rows in sixteens beside each other, too (64 x 1000 x 4096: 28 us without that)
+    if (few <= 16 || many <= 2048) return many >= 32 * 2048 ? launch_rows_of<1, 2, TO>(g, turned, s) : launch_rows_of<1, 1, TO>(g, turned, s);
     if (few <= 32) return many >= 32 * 2048 ? launch_rows_of<2, 2, TO>(g, turned, s) : launch_rows_of<2, 1, TO>(g, turned, s);
     return many >= 32 * 2048 ? launch_rows_of<4, 2, TO>(g, turned, s) : launch_rows_of<4, 1, TO>(g, turned, s);
 }
@@ -629,8 +654,10 @@ extern "C" {
 size_t wpsgd_block_matmul_workspace(int64_t rows_a, int64_t rows_b, int64_t cols)
 {
     if (rows_a <= 0 || rows_b <= 0 || cols <= 0) return 0;
-    const MatmulPlan p = plan_matmul(rows_a, rows_b, (cols + 127) / 128, false, false);
-    return p.parts > 1 ? ((size_t)p.parts * rows_a * rows_b * sizeof(float) + 255) & ~(size_t)255 : 0;
+    // (whatever the results' type)
+    const int64_t blocks = (cols + 127) / 128;
+    const size_t a = parts_bytes(plan_matmul(rows_a, rows_b, blocks, true, false), rows_a, rows_b), b = parts_bytes(plan_matmul(rows_a, rows_b, blocks, false, false), rows_a, rows_b);
+    return a > b ? a : b;
 }
 
 int wpsgd_block_matmul(const wpsgd_blocks *A, const wpsgd_blocks *B, void *out, int64_t ld_out, wpsgd_dtype dtype, void *workspace, size_t workspace_bytes,
@@ -648,7 +675,7 @@ int wpsgd_block_matmul(const wpsgd_blocks *A, const wpsgd_blocks *B, void *out, 
     MatmulArgs g{static_cast<const uint8_t *>(A->codes), static_cast<const uint8_t *>(B->codes), static_cast<const uint8_t *>(A->exps),
                  static_cast<const uint8_t *>(B->exps), A->ld, B->ld, A->ld_exps, B->ld_exps, A->rows, B->rows, (int)((A->cols + 127) / 128), out, ld_out, 0};
     const bool f32 = dtype == WPSGD_F32;
-    const MatmulPlan p = plan_matmul(g.M, g.N, g.blocks, !f32, wide(g.lda, g.lde_a) || wide(g.ldb, g.lde_b));
+    const MatmulPlan p = plan_matmul(g.M, g.N, g.blocks, f32, wide(g.lda, g.lde_a) || wide(g.ldb, g.lde_b));
     hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t e = hipSuccess;
     if (p.kind == MatmulPlan::Rows) {

@@ -1,6 +1,6 @@
 // Softmax cross-entropy of a batch of scores, with its gradient:
 //   loss_i = r_i (log sum_c exp(z_ic) - z_it),   grad_ic = scale r_i (exp(z_ic - m_i) / s_i - [c = t]),   m_i the row's maximum, s_i = sum_c exp(z_ic - m_i).
-// One workgroup owns a row; the maximum and the sum are carried together in fp32 (a thread's running sum is rescaled when its maximum grows).
+// Statistics are fp32.
 #include "class_ops.h"
 
 namespace wpsgd {
@@ -19,91 +19,143 @@ struct LossArgs {
 constexpr float kLog2e = 1.44269504088896340736f;
 __device__ inline float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }   // x <= 0
 
-// (m, s) of two parts of a row; a part without a finite maximum has s = 0 or NaN
-__device__ inline void join(float &m, float &s, float m2, float s2)
+// The row waits in registers between its statistics and its gradient, V vectors of sixteen bytes to a thread, so that it is read once; NT threads to a row, 256 / NT
+// rows to a workgroup where that is more than one.  LONG: what a row has beyond 16 NT V bytes is read again for the gradient.  Bound by memory: 8192 x 65536
+// bfloat16 reads and writes 1 GiB each.
+template <typename T, int NT, int V, bool LONG>
+__global__ __launch_bounds__(NT < 256 ? 256 : NT) void softmax_row_kernel(LossArgs a)
 {
-    const float top = fmaxf(m, m2);
-    const float a = m == top ? s : s * exp_of(m - top), b = m2 == top ? s2 : s2 * exp_of(m2 - top);
-    m = top;
-    s = a + b;
-}
-
-template <typename T, int NT>
-__global__ __launch_bounds__(NT) void softmax_row_kernel(LossArgs a)
-{
-    constexpr int E = Elem<T>::kPer16;
-    __shared__ float part[2][NT / 64];
-    const int64_t row = blockIdx.x;
-    const int t = threadIdx.x;
+    constexpr int E = Elem<T>::kPer16, kRows = NT < 256 ? 256 / NT : 1, kWaves = NT / 64;
+    constexpr float kInf = __builtin_inff();
+    __shared__ float part[2][kWaves];
+    const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / NT;
+    if (kRows > 1 && row >= a.n) return;                                          // (whole waves)
+    const int t = threadIdx.x % NT;
     const T *z = static_cast<const T *>(a.z) + row * a.ld;
     T *g = a.grad ? static_cast<T *>(a.grad) + row * a.ld_grad : nullptr;
     const int64_t label = a.labels[row];
     const float r = a.row_weights ? a.row_weights[row] : 1.0f;
-    const int64_t vectors = a.c / E, tail = a.c - vectors * E;
-    const bool counts = label >= 0 && r != 0.0f;
-    if (counts) {
-        float m = -__builtin_inff(), s = 0.0f;
-        for (int64_t v = t; v < vectors; v += NT) {
-            const Bytes16 q = load16(z + v * E);
-            float top = m;
-#pragma unroll
-            for (int j = 0; j < E; ++j) top = fmaxf(top, Elem<T>::get(q.w, j));
-            const float base = top == -__builtin_inff() ? 0.0f : top;
-            s = s * exp_of(m - base);
-#pragma unroll
-            for (int j = 0; j < E; ++j) s += exp_of(Elem<T>::get(q.w, j) - base);
-            m = top;
-        }
-        if (t < tail) {
-            const float x = Elem<T>::load(z + vectors * E + t);
-            join(m, s, fmaxf(x, -__builtin_inff()), x == -__builtin_inff() ? 0.0f : x - x + 1.0f);
-        }
-        for (int d = 1; d < 64; d *= 2) {
-            const float m2 = __shfl_xor(m, d), s2 = __shfl_xor(s, d);
-            join(m, s, m2, s2);
-        }
-        if ((t & 63) == 0) { part[0][t >> 6] = m; part[1][t >> 6] = s; }
-        __syncthreads();
-        m = part[0][0];
-        s = part[1][0];
-#pragma unroll
-        for (int w = 1; w < NT / 64; ++w) join(m, s, part[0][w], part[1][w]);
-        const bool empty = m == -__builtin_inff() && s == 0.0f;
-        const float bad = label >= a.c ? __builtin_nanf("") : 0.0f;              // no such class: loss and gradient say so
-        if (t == 0) a.loss[row] = label >= a.c ? bad : empty ? __builtin_inff() : (m - Elem<T>::load(z + label) + logf(s)) * r;
+    const int c = (int)a.c, vectors = c / E, tail = c - vectors * E;
+    if (label < 0 || r == 0.0f) {
+        if (t == 0) a.loss[row] = 0.0f;
         if (!g) return;
-        __syncthreads();                                                          // (the label's score is read before it may be overwritten)
-        const float f = a.scale * r, over = (empty ? 0.0f : f / s) + bad, base = empty ? 0.0f : m;
-        for (int64_t v = t; v < vectors; v += NT) {
-            const Bytes16 q = load16(z + v * E);
-            float p[E];
-#pragma unroll
-            for (int j = 0; j < E; ++j) p[j] = exp_of(Elem<T>::get(q.w, j) - base) * over;
-            if (label >= v * E && label < (v + 1) * E && !empty) {
-#pragma unroll
-                for (int j = 0; j < E; ++j) p[j] = j == (int)(label - v * E) ? p[j] - f : p[j];
-            }
-            Bytes16 o;
-            if constexpr (E == 8) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) o.w[j] = bf16_pack(p[2 * j], p[2 * j + 1]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) o.w[j] = __float_as_uint(p[j]);
-            }
-            store16(g + v * E, o);
-        }
-        if (t < tail) {
-            const int64_t at = vectors * E + t;
-            const float p = exp_of(Elem<T>::load(z + at) - base) * over;
-            Elem<T>::put(g + at, at == label && !empty ? p - f : p);
-        }
+        for (int v = t; v < vectors; v += NT) store16(g + (int64_t)v * E, Bytes16{{0, 0, 0, 0}});
+        if (t < tail) Elem<T>::put(g + (int64_t)vectors * E + t, 0.0f);
         return;
     }
-    if (t == 0) a.loss[row] = 0.0f;
+    Bytes16 q[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int at = v * NT + t;
+        q[v] = at < vectors ? load16(z + (int64_t)at * E) : E == 8 ? Bytes16{{0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u}}
+                                                                   : Bytes16{{0xFF800000u, 0xFF800000u, 0xFF800000u, 0xFF800000u}};      // -inf
+    }
+    const float last = t < tail ? Elem<T>::load(z + (int64_t)vectors * E + t) : -kInf;
+    const float z_label = t == 0 && label < a.c ? Elem<T>::load(z + label) : 0.0f;
+    // the packed words are what waits: without this the compiler keeps what it has unpacked beside them, twice the registers
+    auto pack = [&]() {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(q[v].w[j]));
+    };
+    float m = last;                                                               // (fmaxf passes over a NaN, which then shows in the sum)
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int j = 0; j < E; ++j) m = fmaxf(m, Elem<T>::get(q[v].w, j));
+    m = fmaxf(m, -kInf);
+    float s = 0.0f;
+    if constexpr (LONG) {
+        for (int v = V * NT + t; v < vectors; v += NT) {
+            const Bytes16 more = load16(z + (int64_t)v * E);
+            float top = m;
+#pragma unroll
+            for (int j = 0; j < E; ++j) top = fmaxf(top, Elem<T>::get(more.w, j));
+            const float base = top == -kInf ? 0.0f : top;
+            s = s * exp_of(m - base);
+#pragma unroll
+            for (int j = 0; j < E; ++j) s += exp_of(Elem<T>::get(more.w, j) - base);
+            m = top;
+        }
+    }
+    pack();
+    const float own = m;                                                          // what s is relative to
+    m = wave_max(m);
+    if constexpr (kWaves > 1) {
+        if ((t & 63) == 0) part[0][t >> 6] = m;
+        __syncthreads();
+        m = part[0][0];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) m = fmaxf(m, part[0][w]);
+    }
+    const bool none = m == -kInf;                                                 // every score is -inf or NaN
+    const float base = none ? 0.0f : m;
+    if constexpr (LONG) s = own == -kInf ? s : s * exp_of(own - base);
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int j = 0; j < E; ++j) s += exp_of(Elem<T>::get(q[v].w, j) - base);
+    s += exp_of(last - base);
+    pack();
+    s = wave_sum(s);
+    if constexpr (kWaves > 1) {
+        if ((t & 63) == 0) part[1][t >> 6] = s;
+        __syncthreads();
+        s = part[1][0];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) s += part[1][w];
+    }
+    const bool empty = none && s == 0.0f;
+    const float bad = label >= a.c ? __builtin_nanf("") : 0.0f;                   // no such class: loss and gradient say so
+    if (t == 0) a.loss[row] = label >= a.c ? bad : empty ? kInf : (m - z_label + logf(s)) * r;
     if (!g) return;
-    for (int64_t v = t; v < vectors; v += NT) store16(g + v * E, Bytes16{{0, 0, 0, 0}});
-    if (t < tail) Elem<T>::put(g + vectors * E + t, 0.0f);
+    const float f = a.scale * r, over = (empty ? 0.0f : f / s) + bad;
+    const int at_label = empty || label >= a.c ? -1 : (int)label;
+    auto gradient = [&](int v, const Bytes16 &x) {
+        float p[E];
+#pragma unroll
+        for (int j = 0; j < E; ++j) p[j] = exp_of(Elem<T>::get(x.w, j) - base) * over;
+        if (at_label / E == v && at_label >= 0) {
+#pragma unroll
+            for (int j = 0; j < E; ++j) p[j] = at_label % E == j ? p[j] - f : p[j];
+        }
+        Bytes16 o;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (E == 8) o.w[j] = bf16_pack(p[2 * j], p[2 * j + 1]);
+            else o.w[j] = __float_as_uint(p[j]);
+        }
+        store16(g + (int64_t)v * E, o);
+    };
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        if (v * NT + t < vectors) gradient(v * NT + t, q[v]);
+    if constexpr (LONG) {
+        for (int v = V * NT + t; v < vectors; v += NT) gradient(v, load16(z + (int64_t)v * E));
+    }
+    if (t < tail) {
+        const float p = exp_of(last - base) * over;
+        Elem<T>::put(g + (int64_t)vectors * E + t, at_label == vectors * E + t ? p - f : p);
+    }
+}
+
+template <typename T>
+static hipError_t launch_loss(const LossArgs &a, hipStream_t s)
+{
+    const int64_t vectors = a.c / Elem<T>::kPer16;
+    const auto run = [&](auto kernel, int64_t groups, int threads) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(threads), 0, s, a);
+        return hipGetLastError();
+    };
+    // the fewest threads whose registers hold a row; rows that half the registers of a compute unit cannot hold are its only one
+    if (vectors <= 64 * 4) return run(softmax_row_kernel<T, 64, 4, false>, (a.n + 3) / 4, 256);
+    if (vectors <= 256 * 4) return run(softmax_row_kernel<T, 256, 4, false>, a.n, 256);
+    if (vectors <= 256 * 8) return run(softmax_row_kernel<T, 256, 8, false>, a.n, 256);
+    if (vectors <= 256 * 16) return run(softmax_row_kernel<T, 256, 16, false>, a.n, 256);
+    if (vectors <= 512 * 16) return run(softmax_row_kernel<T, 512, 16, false>, a.n, 512);
+    if (vectors <= 1024 * 16) return run(softmax_row_kernel<T, 1024, 16, false>, a.n, 1024);
+    return run(softmax_row_kernel<T, 1024, 16, true>, a.n, 1024);
 }
 
 }  // namespace wpsgd
@@ -133,9 +185,7 @@ int wpsgd_softmax_loss(const void *Z, int64_t n, int64_t classes, int64_t ld, wp
     if (workspace_bytes < need) return WPSGD_WORKSPACE_TOO_SMALL;
     const LossArgs a{Z, n, classes, ld, labels, row_weights, (float)scale, loss, grad, ld_grad};
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (dtype == WPSGD_F32) hipLaunchKernelGGL((softmax_row_kernel<float, 256>), dim3((unsigned)n), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((softmax_row_kernel<uint16_t, 256>), dim3((unsigned)n), dim3(256), 0, s, a);
-    const hipError_t e = hipGetLastError();
+    const hipError_t e = dtype == WPSGD_F32 ? launch_loss<float>(a, s) : launch_loss<uint16_t>(a, s);
     return e == hipSuccess ? WPSGD_OK : hip_fail(e);
 }
 

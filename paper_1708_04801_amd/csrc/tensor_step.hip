@@ -4,7 +4,7 @@
 //   c    = min(1, max_norm / norm)
 //   w   <- (1 - eta lambda) w - eta c g           a norm that is not finite changes nothing
 //
-// A list's table, made once, cuts the tensors into chunks of at most kChunk elements, so that the kernels see one flat sequence of equal pieces
+// A list's table, made once, cuts the tensors into chunks of some thousand elements, so that the kernels see one flat sequence of equal pieces
 // whatever the tensors' number and sizes.
 #include <cmath>
 #include <vector>
@@ -13,7 +13,10 @@
 
 namespace wpsgd {
 
-constexpr int kChunk = 16384;
+// Elements of a chunk.  A small model in small chunks, so that it spreads over the chip (3M elements: 16384 to a chunk 5.0 us for the norm and 8.8 for the step,
+// 2048 to a chunk 3.4 and 4.4); a large one in large ones, of which a workgroup has many and asks for several vectors at a time.
+constexpr int kLargeChunk = 16384, kSmallChunk = 2048;
+constexpr int64_t kSmallModel = 8 << 20;
 constexpr int kNormGroups = 1024;        // partial sums at most, one per workgroup
 
 struct Chunk {
@@ -25,19 +28,25 @@ struct Chunk {
 };
 static_assert(sizeof(Chunk) == 32, "two to a cache line quarter");
 
+constexpr int kAtOnce = 4;               // vectors on their way
+
 template <typename T>
 __device__ inline double sum_squares(const T *g, int n)
 {
     constexpr int E = Elem<T>::kPer16;
     const int vectors = n / E;
     double s = 0.0;
-    for (int v = threadIdx.x; v < vectors; v += 256) {
-        const Bytes16 q = load16(g + v * E);
+    for (int v0 = threadIdx.x; v0 < vectors; v0 += 256 * kAtOnce) {
+        Bytes16 q[kAtOnce];
 #pragma unroll
-        for (int j = 0; j < E; ++j) {
-            const double x = (double)Elem<T>::get(q.w, j);
-            s = fma(x, x, s);
-        }
+        for (int u = 0; u < kAtOnce; ++u) q[u] = v0 + u * 256 < vectors ? load16(g + (v0 + u * 256) * E) : Bytes16{{0, 0, 0, 0}};
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                const double x = (double)Elem<T>::get(q[u].w, j);
+                s = fma(x, x, s);
+            }
     }
     const int at = vectors * E + threadIdx.x;
     if (at < n) {
@@ -98,35 +107,48 @@ __device__ inline float stepped(float w, float g, double shrink, double factor) 
 template <typename T>
 __device__ inline void step_chunk(const Chunk &c, double shrink, double factor)
 {
-    constexpr int E = Elem<T>::kPer16;
+    constexpr int E = Elem<T>::kPer16, U = 16 / E;
     const T *g = static_cast<const T *>(c.g);
     const int vectors = c.n / E;
-    for (int v = threadIdx.x; v < vectors; v += 256) {
-        const Bytes16 q = load16(g + v * E);
+    for (int v0 = threadIdx.x; v0 < vectors; v0 += 256 * U) {
+        Bytes16 q[U], w[U][E / 4];
 #pragma unroll
-        for (int h = 0; h < E / 4; ++h) {
-            float *p = c.w + v * E + h * 4;
-            Bytes16 w = load16(p);
+        for (int u = 0; u < U; ++u) {
+            const int v = v0 + u * 256 < vectors ? v0 + u * 256 : v0;
+            q[u] = load16(g + v * E);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) w.w[j] = __float_as_uint(stepped(__uint_as_float(w.w[j]), Elem<T>::get(q.w, h * 4 + j), shrink, factor));
-            store16(p, w);
+            for (int h = 0; h < E / 4; ++h) w[u][h] = load16(c.w + v * E + h * 4);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int v = v0 + u * 256;
+            if (v >= vectors) break;
+#pragma unroll
+            for (int h = 0; h < E / 4; ++h) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    w[u][h].w[j] = __float_as_uint(stepped(__uint_as_float(w[u][h].w[j]), Elem<T>::get(q[u].w, h * 4 + j), shrink, factor));
+                store16(c.w + v * E + h * 4, w[u][h]);
+            }
         }
     }
     const int at = vectors * E + threadIdx.x;
     if (at < c.n) Elem<float>::put(c.w + at, stepped(Elem<float>::load(c.w + at), Elem<T>::load(g + at), shrink, factor));
 }
 
+// (Asking for the first chunk's vectors in front of the norm gains nothing: 9.2 us instead of 8.1 for 3M elements, 635 instead of 625 for 268M.)
 __global__ __launch_bounds__(256) void clipped_step_kernel(StepArgs a)
 {
     __shared__ double part[4];
     const double norm = sqrt(total_of(a.partials, a.groups, part));
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)norm;
     if (!(norm < __builtin_inf())) return;
-    const double factor = norm > a.max_norm ? a.eta * (a.max_norm / norm) : a.eta, shrink = a.shrink;
-    for (int64_t i = blockIdx.x; i < a.count; i += gridDim.x) {
+    const double factor = norm > a.max_norm ? a.eta * (a.max_norm / norm) : a.eta;
+    // from the end: what the norm has read last may still be in the caches
+    for (int64_t i = a.count - 1 - blockIdx.x; i >= 0; i -= gridDim.x) {
         const Chunk c = a.chunks[i];
-        if (c.dtype == WPSGD_BF16) step_chunk<uint16_t>(c, shrink, factor);
-        else step_chunk<float>(c, shrink, factor);
+        if (c.dtype == WPSGD_BF16) step_chunk<uint16_t>(c, a.shrink, factor);
+        else step_chunk<float>(c, a.shrink, factor);
     }
 }
 
@@ -156,7 +178,7 @@ __global__ __launch_bounds__(256) void clip_kernel(StepArgs a)
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)norm;
     if (!(norm < __builtin_inf()) || norm <= a.max_norm) return;             // nothing to scale: nothing is written
     const double factor = a.max_norm / norm;
-    for (int64_t i = blockIdx.x; i < a.count; i += gridDim.x) {
+    for (int64_t i = a.count - 1 - blockIdx.x; i >= 0; i -= gridDim.x) {
         const Chunk c = a.chunks[i];
         if (c.dtype == WPSGD_BF16) scale_chunk<uint16_t>(c, factor);
         else scale_chunk<float>(c, factor);
@@ -179,6 +201,20 @@ static hipError_t launch_square_sums(const wpsgd_tensor_list *l, double *partial
     return hipGetLastError();
 }
 
+static int64_t chunk_of(int64_t elements) { return elements <= kSmallModel ? kSmallChunk : kLargeChunk; }
+// -1 for descriptions that cannot be
+static int64_t count_chunks(const wpsgd_tensor *tensors, int64_t count)
+{
+    if (count < 0 || (count > 0 && !tensors)) return -1;
+    int64_t elements = 0, chunks = 0;
+    for (int64_t i = 0; i < count; ++i) {
+        if (tensors[i].n < 0 || tensors[i].n > (1LL << 44) || elements > (1LL << 44)) return -1;
+        elements += tensors[i].n;
+    }
+    for (int64_t i = 0; i < count; ++i) chunks += (tensors[i].n + chunk_of(elements) - 1) / chunk_of(elements);
+    return chunks;
+}
+
 static unsigned step_groups(int64_t chunks) { return (unsigned)(chunks < 1 ? 1 : chunks < 4096 ? chunks : 4096); }
 
 }  // namespace wpsgd
@@ -189,23 +225,17 @@ extern "C" {
 
 size_t wpsgd_tensor_list_bytes(const wpsgd_tensor *tensors, int64_t count)
 {
-    if (count < 0 || (count > 0 && !tensors)) return 0;
-    int64_t chunks = 0;
-    for (int64_t i = 0; i < count; ++i) {
-        if (tensors[i].n < 0 || tensors[i].n > (1LL << 46)) return 0;
-        chunks += (tensors[i].n + kChunk - 1) / kChunk;
-        if (chunks > (1LL << 32)) return 0;
-    }
-    return ((size_t)(chunks < 1 ? 1 : chunks) * sizeof(Chunk) + 255) & ~(size_t)255;
+    const int64_t chunks = count_chunks(tensors, count);
+    return chunks < 0 ? 0 : ((size_t)(chunks < 1 ? 1 : chunks) * sizeof(Chunk) + 255) & ~(size_t)255;
 }
 
 int wpsgd_tensor_list_make(const wpsgd_tensor *tensors, int64_t count, void *table, size_t table_bytes, wpsgd_tensor_list *list, void *stream)
 {
-    const size_t need = wpsgd_tensor_list_bytes(tensors, count);
-    if (need == 0 || !list || !table || (uintptr_t)table % 256 != 0) return WPSGD_INVALID_ARG;
-    if (table_bytes < need) return WPSGD_WORKSPACE_TOO_SMALL;
+    const int64_t chunks = count_chunks(tensors, count);
+    if (chunks < 0 || !list || !table || (uintptr_t)table % 256 != 0) return WPSGD_INVALID_ARG;
+    if (table_bytes < wpsgd_tensor_list_bytes(tensors, count)) return WPSGD_WORKSPACE_TOO_SMALL;
     bool weights = true;
-    int64_t elements = 0, chunks = 0;
+    int64_t elements = 0;
     for (int64_t i = 0; i < count; ++i) {
         const wpsgd_tensor &t = tensors[i];
         if (t.dtype != WPSGD_F32 && t.dtype != WPSGD_BF16) return WPSGD_INVALID_ARG;
@@ -213,16 +243,16 @@ int wpsgd_tensor_list_make(const wpsgd_tensor *tensors, int64_t count, void *tab
         if (!t.grad || (uintptr_t)t.grad % (t.dtype == WPSGD_F32 ? 4 : 2) != 0 || (uintptr_t)t.weight % 4 != 0) return WPSGD_INVALID_ARG;
         weights = weights && t.weight;
         elements += t.n;
-        chunks += (t.n + kChunk - 1) / kChunk;
     }
     try {
+        const int64_t each = chunk_of(elements);
         std::vector<Chunk> host;
         host.reserve((size_t)chunks);
         for (int64_t i = 0; i < count; ++i) {
             const wpsgd_tensor &t = tensors[i];
-            for (int64_t at = 0; at < t.n; at += kChunk)
+            for (int64_t at = 0; at < t.n; at += each)
                 host.push_back(Chunk{static_cast<char *>(t.grad) + at * (t.dtype == WPSGD_F32 ? 4 : 2), t.weight ? t.weight + at : nullptr,
-                                     (int32_t)(t.n - at < kChunk ? t.n - at : kChunk), (int32_t)t.dtype, 0});
+                                     (int32_t)(t.n - at < each ? t.n - at : each), (int32_t)t.dtype, 0});
         }
         if (chunks > 0) {
             const int rc = upload(table, host.data(), host.size() * sizeof(Chunk), static_cast<hipStream_t>(stream));

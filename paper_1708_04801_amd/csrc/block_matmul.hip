@@ -199,8 +199,8 @@ __device__ inline void tile_of(uint32_t id, uint32_t count, uint32_t tiles_m, ui
 
 // Large products.  A workgroup of four waves, two by two, has 64 TM x 64 TN results, a wave 32 TM x 32 TN; blocks of 128 along the sum.
 //
-// Rows land in LDS by themselves, eight rows of 128 bytes to an instruction.  Sixteen bytes q of row r lie at place q ^ (r mod 8) of the row, so that the lanes of
-// an LDS access that read the same piece of neighbouring rows meet different banks; the loads fetch in that order.  Rows behind the last repeat it.  Each
+// Rows land in LDS by themselves, eight rows of 128 bytes to an instruction.  Sixteen bytes q of row r lie at place q ^ (r / 2 mod 8) of the row, so that any sixteen lanes
+// that read the same piece of rows which differ modulo 16 meet all banks once (with r mod 8 half of the LDS cycles were conflicts); the loads fetch in that order.  Rows behind the last repeat it.  Each
 // row's exponent bytes come four blocks at a time, a word a row, into two buffers in turn.
 template <int TM, int TN>
 struct Tile {
@@ -230,19 +230,19 @@ struct Tile {
         left_n = (int)(g.N - j0 < BN ? g.N - j0 : BN);
         ra = resource(g.a + i0 * g.lda + (int64_t)first * 128);
         rb = resource(g.b + j0 * g.ldb + (int64_t)first * 128);
-        const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
+        const auto piece = [&](int row) { return ((lane & 7) ^ ((row >> 1) & 7)) * 16; };     // of a row of LDS
         constexpr int kUnit = 2 * ROWS, kUnits = BM / kUnit, kEach = LA / kUnits;      // rows of a unit, units, a wave's loads for one
 #pragma unroll
         for (int t = 0; t < LA; ++t) {
             const int in = (wave * kEach + t % kEach) * 8 + (lane >> 3);            // row of the unit
             const int r = (in / ROWS) * (BM / 2) + (t / kEach) * ROWS + in % ROWS;
-            from_a[t] = (r < left_m ? r : left_m - 1) * (int)g.lda + piece;
+            from_a[t] = (r < left_m ? r : left_m - 1) * (int)g.lda + piece(in);
             asm volatile("" : "+v"(from_a[t]));            // (one register: the compiler's product has two)
         }
 #pragma unroll
         for (int t = 0; t < LB; ++t) {
             const int r = (wave * LB + t) * 8 + (lane >> 3);
-            from_b[t] = (r < left_n ? r : left_n - 1) * (int)g.ldb + piece;
+            from_b[t] = (r < left_n ? r : left_n - 1) * (int)g.ldb + piece(r);
             asm volatile("" : "+v"(from_b[t]));
         }
         // words of exponents: A's rows, then B's, 64 to an instruction, a wave's share in one or two
@@ -356,7 +356,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM * TN > 8
         else fetch_to_lds(tile.rb, to + G::BM * 128 + (wave * G::LB + n - G::LA) * 1024, tile.from_b[n - G::LA], b * 128);
     };
     auto read = [&](int row, int b, int part) -> uint4 {
-        return *reinterpret_cast<const uint4 *>(lds + (b & 1) * kStage + row * 128 + (((part * 2 + half) ^ (r & 7)) * 16));
+        return *reinterpret_cast<const uint4 *>(lds + (b & 1) * kStage + row * 128 + (((part * 2 + half) ^ ((r >> 1) & 7)) * 16));
     };
     auto scale = [&](int row, int b) -> float {
         return power_of(lds[2 * kStage + ((b >> 2) & 1) * G::kExps + row * 4 + (b & 3)]);
@@ -481,7 +481,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
         i32x8 v;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const uint4 q = *reinterpret_cast<const uint4 *>(p + (((k * 4 + h * 2 + half) ^ (r & 7)) * 16));
+            const uint4 q = *reinterpret_cast<const uint4 *>(p + (((k * 4 + h * 2 + half) ^ ((r >> 1) & 7)) * 16));
             v[h * 4] = (int)q.x; v[h * 4 + 1] = (int)q.y; v[h * 4 + 2] = (int)q.z; v[h * 4 + 3] = (int)q.w;
         }
         return v;

@@ -83,3 +83,22 @@ def test_steps_bring_the_loss_down():
     s = Step(seed=2)
     losses = [float(s()[2].double().mean()) for _ in range(30)]
     assert all(b < a for a, b in zip(losses, losses[1:]))
+
+
+def test_the_workers_example():
+    """unequal workers learn, and the loss of their weighted average is under the weighted average of their losses, as the loss is convex (8-bit
+    rows and class vectors give and take 1 % of it)"""
+    import importlib.util
+    import math
+    import os
+
+    from conftest import ROOT
+    spec = importlib.util.spec_from_file_location("many_class_workers", os.path.join(ROOT, "examples", "many_class_workers.py"))
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    start, workers, average, answers, labels = example.train(m=4096, d=256, classes=300, heads=2, steps=(30, 30, 20, 10), batch=256)
+    assert abs(start - math.log(300)) < 1e-4                      # zero class vectors: every class alike
+    a = api.wpsgd_weights([30, 30, 20, 10], 2.0, 1e-4)
+    assert all(v < start for v in workers) and average < 1.01 * sum(x * v for x, v in zip(a, workers)) and average < start
+    assert answers.shape == labels.shape == (2048, 2) and bool(((answers >= 0) & (answers < 300)).all())
+    assert float((answers == labels).double().mean()) > 1 / 300 + 5 * math.sqrt(1 / 300 / answers.numel())      # more often than by chance

@@ -303,7 +303,7 @@ typedef struct wpsgd_blocks {
     int64_t rows, cols;        /* 0 <= cols <= 2^31                                                       */
     void *codes;               /* DEVICE, one byte each, 16-byte aligned                                  */
     int64_t ld;                /* row stride in bytes, a multiple of 16, >= 128*ceil(cols/128)            */
-    void *exps;                /* DEVICE, one byte for each block, 4-byte aligned                         */
+    void *exps;                /* DEVICE, one byte (1 .. 254) for each block, 4-byte aligned              */
     int64_t ld_exps;           /* row stride in bytes, a multiple of 4, >= ceil(cols/128)                 */
 } wpsgd_blocks;
 
@@ -317,7 +317,9 @@ typedef struct wpsgd_blocks {
  * Errors: INVALID_ARG, UNSUPPORTED (CSR; more than 2^31 - 1 workgroups), HIP_ERROR.                                    */
 int wpsgd_quantize(const wpsgd_matrix *X, const int64_t *rows, int64_t n, int transpose, const wpsgd_blocks *out, void *stream);
 
-/* out[i*ld_out + j] = sum_c A(i, c) * B(j, c), for all rows i of A and j of B: summed in fp32, rounded once to dtype.
+/* out[i*ld_out + j] = sum_c A(i, c) * B(j, c), for all rows i of A and j of B: summed in fp32, rounded once to dtype.  Large products
+ * to bfloat16 go through the 8-bit matrix instructions, which of a few products at a time keep what lies within 2^14 of the
+ * largest: 1e-5 to 7e-5 of a result's usual size, where the type's own rounding is 2e-3.  Results are NaN where a row has a NaN.
  * With x the rows of a batch (n x d), W the class vectors (classes x d) and G the loss gradient (n x classes):
  *   scores              A = x, B = W                 gradient of W      A = G transposed, B = x transposed
  *   gradient of x       A = G, B = W transposed      (transposed: as wpsgd_quantize makes it)
@@ -338,16 +340,14 @@ int wpsgd_block_matmul(const wpsgd_blocks *A, const wpsgd_blocks *B, void *out, 
  *   labels       DEVICE, n                    row_weights  DEVICE, n (r_i), or NULL for ones
  *   loss         DEVICE out, n fp32           grad         DEVICE out, dtype as Z, row stride ld_grad; NULL: not wanted.
  *                                             It may be Z itself (with ld_grad = ld), else it may not overlap it.
- *   workspace    DEVICE scratch of at least wpsgd_softmax_loss_workspace(...) bytes, 256-byte aligned (NULL where that is 0)
- * Statistics are fp32; the result does not depend on timing.  Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, HIP_ERROR.      */
-size_t wpsgd_softmax_loss_workspace(int64_t n, int64_t classes, wpsgd_dtype dtype);
+ * Statistics are fp32; the result does not depend on timing.  Errors: INVALID_ARG, HIP_ERROR.                          */
 int wpsgd_softmax_loss(const void *Z, int64_t n, int64_t classes, int64_t ld, wpsgd_dtype dtype, const int64_t *labels,
-                       const float *row_weights, double scale, float *loss, void *grad, int64_t ld_grad,
-                       void *workspace, size_t workspace_bytes, void *stream);
+                       const float *row_weights, double scale, float *loss, void *grad, int64_t ld_grad, void *stream);
 
 /* A model that lies in many tensors: gradients in fp32 or bfloat16, weights in fp32.  A list is made once from HOST
  * descriptions (this call copies them, so it cannot be recorded into a graph; the others can) and stays valid while the
- * tensors stay where they are.  `table` is DEVICE memory of wpsgd_tensor_list_bytes(...), 256-byte aligned, that belongs to
+ * tensors stay where they are (no two of a list may overlap).  The descriptions are queued on `stream`: a call on another one has to be
+ * ordered behind it.  `table` is DEVICE memory of wpsgd_tensor_list_bytes(...), 256-byte aligned, that belongs to
  * the list from then on.  wpsgd_tensor_list_bytes returns 0 for arguments the call would refuse.                   */
 typedef struct wpsgd_tensor {
     void *grad;                /* DEVICE, n elements of dtype                                             */
@@ -368,7 +368,8 @@ int wpsgd_tensor_list_make(const wpsgd_tensor *tensors, int64_t count, void *tab
  * one fp32; all three calls write it, and none depends on timing.
  *   wpsgd_clip_grads     g <- g * max_norm / norm  where norm is finite and over max_norm; else nothing is written
  *   wpsgd_clipped_step   w <- (1 - eta*lambda) * w - eta * min(1, max_norm / norm) * g   (g stays as it is); a norm that
- *                        is not finite changes no weight.  max_norm may be infinite: no clipping.
+ *                        is not finite changes no weight (one that only fp32 cannot hold is written as inf, and the step is
+ *                        taken, in fp64).  max_norm may be infinite: no clipping.
  *   workspace  DEVICE scratch of at least wpsgd_grad_norm_workspace(list) bytes, 256-byte aligned
  * Errors: INVALID_ARG (eta, lambda as for wpsgd_run_chains; max_norm > 0), WORKSPACE_TOO_SMALL, HIP_ERROR.              */
 size_t wpsgd_grad_norm_workspace(const wpsgd_tensor_list *list);
@@ -397,12 +398,10 @@ typedef struct wpsgd_draw_rule {
  *   u        DEVICE, n numbers in [0, 1)
  *   drawn    DEVICE out, n; -1 for a row without a class that can be drawn
  *   probs    DEVICE out, n, or NULL: q / Q of the class drawn (0 beside -1)
- *   workspace DEVICE scratch of at least wpsgd_draw_classes_workspace(...) bytes, 256-byte aligned (NULL where that is 0)
- * Errors: INVALID_ARG (temperature >= 0, min_p <= 1, neither NaN), WORKSPACE_TOO_SMALL, HIP_ERROR.                      */
-size_t wpsgd_draw_classes_workspace(int64_t n, int64_t classes, wpsgd_dtype dtype);
+ * A row's setting cannot be refused: a temperature that is no positive number counts as 0, a min_p over 1 or NaN as 1.
+ * Errors: INVALID_ARG (temperature >= 0, min_p <= 1, neither NaN, nor top_p), UNSUPPORTED, HIP_ERROR.                  */
 int wpsgd_draw_classes(const void *Z, int64_t n, int64_t classes, int64_t ld, wpsgd_dtype dtype, const float *u,
-                       const wpsgd_draw_rule *rule, int64_t *drawn, float *probs,
-                       void *workspace, size_t workspace_bytes, void *stream);
+                       const wpsgd_draw_rule *rule, int64_t *drawn, float *probs, void *stream);
 
 /* ---- diagnostics ---- */
 /* Streaming ceiling probe (not a step of the method): `groups` workgroups of 256 threads each read

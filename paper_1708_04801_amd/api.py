@@ -31,9 +31,9 @@ EXPORTS = [
     "wpsgd_run_spans_workspace", "wpsgd_run_spans", "wpsgd_span_condition", "wpsgd_objective_static",
     "wpsgd_chains_status", "wpsgd_run_delay_chains_workspace", "wpsgd_run_delay_chains",
     "wpsgd_quantize", "wpsgd_block_matmul_workspace", "wpsgd_block_matmul",
-    "wpsgd_softmax_loss_workspace", "wpsgd_softmax_loss", "wpsgd_tensor_list_bytes", "wpsgd_tensor_list_make",
+    "wpsgd_softmax_loss", "wpsgd_tensor_list_bytes", "wpsgd_tensor_list_make",
     "wpsgd_grad_norm_workspace", "wpsgd_grad_norm", "wpsgd_clip_grads", "wpsgd_clipped_step",
-    "wpsgd_draw_classes_workspace", "wpsgd_draw_classes",
+    "wpsgd_draw_classes",
 ]
 
 
@@ -128,9 +128,7 @@ def load():
     L.wpsgd_block_matmul_workspace.argtypes = [i64, i64, i64]
     L.wpsgd_block_matmul_workspace.restype = sz
     L.wpsgd_block_matmul.argtypes = [pb, pb, vp, i64, ci, vp, sz, vp]
-    L.wpsgd_softmax_loss_workspace.argtypes = [i64, i64, ci]
-    L.wpsgd_softmax_loss_workspace.restype = sz
-    L.wpsgd_softmax_loss.argtypes = [vp, i64, i64, i64, ci, vp, vp, f64, vp, vp, i64, vp, sz, vp]
+    L.wpsgd_softmax_loss.argtypes = [vp, i64, i64, i64, ci, vp, vp, f64, vp, vp, i64, vp]
     L.wpsgd_tensor_list_bytes.argtypes = [pt, i64]
     L.wpsgd_tensor_list_bytes.restype = sz
     L.wpsgd_tensor_list_make.argtypes = [pt, i64, vp, sz, pl, vp]
@@ -139,9 +137,7 @@ def load():
     L.wpsgd_grad_norm.argtypes = [pl, vp, vp, sz, vp]
     L.wpsgd_clip_grads.argtypes = [pl, f64, vp, vp, sz, vp]
     L.wpsgd_clipped_step.argtypes = [pl, f64, f64, f64, vp, vp, sz, vp]
-    L.wpsgd_draw_classes_workspace.argtypes = [i64, i64, ci]
-    L.wpsgd_draw_classes_workspace.restype = sz
-    L.wpsgd_draw_classes.argtypes = [vp, i64, i64, i64, ci, vp, ctypes.POINTER(_CDrawRule), vp, vp, vp, sz, vp]
+    L.wpsgd_draw_classes.argtypes = [vp, i64, i64, i64, ci, vp, ctypes.POINTER(_CDrawRule), vp, vp, vp]
     _lib = L
     return L
 
@@ -596,7 +592,7 @@ def wpsgd_block_matmul(A: BlockMatrix, B: BlockMatrix, out: Optional[torch.Tenso
     assert out.is_cuda and out.dtype in _DTYPES and out.shape == (A.rows, B.rows) and (out.numel() == 0 or out.stride(1) == 1)
     L = load()
     p, size, held = _call_workspace(workspace, L.wpsgd_block_matmul_workspace(A.rows, B.rows, A.cols), out.device, stream)
-    rc = L.wpsgd_block_matmul(ctypes.byref(A.c_struct()), ctypes.byref(B.c_struct()), out.data_ptr(), max(out.stride(0), B.rows),
+    rc = L.wpsgd_block_matmul(ctypes.byref(A.c_struct()), ctypes.byref(B.c_struct()), out.data_ptr(), out.stride(0) if A.rows > 1 else max(out.stride(0), B.rows),
                               _DTYPES[out.dtype], p, size, _stream_of(stream, out))
     if rc != OK:
         raise WpsgdError(rc, "wpsgd_block_matmul")
@@ -610,12 +606,8 @@ def _rows_of(Z):
     return n, c, ld if n > 1 else max(ld, c)
 
 
-def wpsgd_softmax_loss_workspace(n, classes, dtype) -> int:
-    return int(load().wpsgd_softmax_loss_workspace(int(n), int(classes), _DTYPES[dtype]))
-
-
 def wpsgd_softmax_loss(Z: torch.Tensor, labels: torch.Tensor, scale=1.0, row_weights: Optional[torch.Tensor] = None,
-                       loss: Optional[torch.Tensor] = None, grad=True, workspace: Optional[torch.Tensor] = None, stream=None):
+                       loss: Optional[torch.Tensor] = None, grad=True, stream=None):
     """(loss, grad): the rows' weighted cross-entropies (float32) and the gradient of scale * sum(loss) with respect to
     the scores Z, in Z's type.  grad: True for a new tensor, a tensor to write (Z itself too), or False for none."""
     n, c, ld = _rows_of(Z)
@@ -634,11 +626,9 @@ def wpsgd_softmax_loss(Z: torch.Tensor, labels: torch.Tensor, scale=1.0, row_wei
         g_ptr = grad.data_ptr()
     else:
         grad, g_ptr, g_ld = None, None, 0
-    L = load()
-    dt = _DTYPES[Z.dtype]
-    p, size, held = _call_workspace(workspace, L.wpsgd_softmax_loss_workspace(n, c, dt), Z.device, stream)
-    rc = L.wpsgd_softmax_loss(Z.data_ptr(), n, c, ld, dt, labels.data_ptr(), row_weights.data_ptr() if row_weights is not None else None,
-                              float(scale), loss.data_ptr(), g_ptr, g_ld, p, size, _stream_of(stream, Z))
+    rc = load().wpsgd_softmax_loss(Z.data_ptr(), n, c, ld, _DTYPES[Z.dtype], labels.data_ptr(),
+                                   row_weights.data_ptr() if row_weights is not None else None, float(scale), loss.data_ptr(), g_ptr, g_ld,
+                                   _stream_of(stream, Z))
     if rc != OK:
         raise WpsgdError(rc, "wpsgd_softmax_loss")
     return loss, grad
@@ -708,13 +698,8 @@ def wpsgd_clipped_step(tensors: TensorList, eta, lam, max_norm=float("inf"), nor
     return _norm_call("wpsgd_clipped_step", tensors, (float(eta), float(lam), float(max_norm)), norm, workspace, stream)
 
 
-def wpsgd_draw_classes_workspace(n, classes, dtype) -> int:
-    return int(load().wpsgd_draw_classes_workspace(int(n), int(classes), _DTYPES[dtype]))
-
-
 def wpsgd_draw_classes(Z: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0,
-                       drawn: Optional[torch.Tensor] = None, probs: Optional[torch.Tensor] = None,
-                       workspace: Optional[torch.Tensor] = None, stream=None):
+                       drawn: Optional[torch.Tensor] = None, probs: Optional[torch.Tensor] = None, stream=None):
     """(drawn, probs): a class for each row of the scores Z (int64, -1 where none can be drawn) and its probability among
     the classes that were kept (float32).  u: float32 in [0, 1).  Each setting is a number, or a tensor with one for each row (float32; top_k int32)."""
     n, c, ld = _rows_of(Z)
@@ -733,11 +718,8 @@ def wpsgd_draw_classes(Z: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=
         probs = torch.empty(n, dtype=torch.float32, device=Z.device)
     assert drawn.is_cuda and drawn.dtype == torch.int64 and drawn.is_contiguous() and drawn.numel() == n
     assert probs.is_cuda and probs.dtype == torch.float32 and probs.is_contiguous() and probs.numel() == n
-    L = load()
-    dt = _DTYPES[Z.dtype]
-    p, size, held = _call_workspace(workspace, L.wpsgd_draw_classes_workspace(n, c, dt), Z.device, stream)
-    rc = L.wpsgd_draw_classes(Z.data_ptr(), n, c, ld, dt, u.data_ptr(), ctypes.byref(rule), drawn.data_ptr(), probs.data_ptr(), p, size,
-                              _stream_of(stream, Z))
+    rc = load().wpsgd_draw_classes(Z.data_ptr(), n, c, ld, _DTYPES[Z.dtype], u.data_ptr(), ctypes.byref(rule), drawn.data_ptr(), probs.data_ptr(),
+                                   _stream_of(stream, Z))
     if rc != OK:
         raise WpsgdError(rc, "wpsgd_draw_classes")
     return drawn, probs

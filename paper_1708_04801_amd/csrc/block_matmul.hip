@@ -628,7 +628,7 @@ static hipError_t launch_rows_of(const MatmulArgs &g, bool turned, hipStream_t s
     int along = 1;
     while (along < kRowWaves && along < kHeldBlocks / MT && groups * panels * along < 2048 && g.blocks >= 2 * along) along *= 2;
     const int64_t grid = (groups * along + kRowWaves - 1) / kRowWaves;
-    if (grid > 0x7FFFFFFFLL || panels > 65535) return hipErrorInvalidValue;
+    if (grid > 0x7FFFFFFFLL || panels > 65535) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL((matmul_rows_kernel<MT, NT, TO>), dim3((unsigned)grid, (unsigned)panels), dim3(64 * kRowWaves), 0, s, g, along, turned);
     return hipGetLastError();
 }
@@ -680,6 +680,7 @@ int wpsgd_block_matmul(const wpsgd_blocks *A, const wpsgd_blocks *B, void *out, 
     hipError_t e = hipSuccess;
     if (p.kind == MatmulPlan::Rows) {
         e = f32 ? launch_rows<float>(g, s) : launch_rows<uint16_t>(g, s);
+        if (e == hipErrorInvalidConfiguration) return WPSGD_UNSUPPORTED;     // more workgroups than a grid has
     } else {
         const int64_t side = p.kind == MatmulPlan::Tile128 ? 128 : 256;
         const int64_t tiles = ((g.M + side - 1) / side) * ((g.N + side - 1) / side);

@@ -840,14 +840,8 @@ using namespace wpsgd;
 
 extern "C" {
 
-size_t wpsgd_draw_classes_workspace(int64_t n, int64_t classes, wpsgd_dtype dtype)
-{
-    (void)n; (void)classes; (void)dtype;
-    return 0;
-}
-
 int wpsgd_draw_classes(const void *Z, int64_t n, int64_t classes, int64_t ld, wpsgd_dtype dtype, const float *u, const wpsgd_draw_rule *rule, int64_t *drawn,
-                       float *probs, void *workspace, size_t workspace_bytes, void *stream)
+                       float *probs, void *stream)
 {
     if (n < 0 || n > 0x7FFFFFFFLL || classes < 1 || (dtype != WPSGD_F32 && dtype != WPSGD_BF16) || !rule) return WPSGD_INVALID_ARG;
     if (!rule->row_temperature && !(rule->temperature >= 0.0f)) return WPSGD_INVALID_ARG;
@@ -856,9 +850,6 @@ int wpsgd_draw_classes(const void *Z, int64_t n, int64_t classes, int64_t ld, wp
     if (n == 0) return WPSGD_OK;
     const size_t elem = dtype == WPSGD_F32 ? 4 : 2;
     if (!Z || !u || !drawn || ld < classes || (uintptr_t)Z % elem != 0) return WPSGD_INVALID_ARG;
-    const size_t need = wpsgd_draw_classes_workspace(n, classes, dtype);
-    if (need && (!workspace || (uintptr_t)workspace % 256 != 0)) return WPSGD_INVALID_ARG;
-    if (workspace_bytes < need) return WPSGD_WORKSPACE_TOO_SMALL;
     const DrawArgs a{Z, n, classes, ld, u, *rule, drawn, probs};
     hipStream_t s = static_cast<hipStream_t>(stream);
     const hipError_t e = dtype == WPSGD_F32 ? launch_draw<float>(a, s) : launch_draw<uint16_t>(a, s);

@@ -164,14 +164,8 @@ using namespace wpsgd;
 
 extern "C" {
 
-size_t wpsgd_softmax_loss_workspace(int64_t n, int64_t classes, wpsgd_dtype dtype)
-{
-    (void)n; (void)classes; (void)dtype;
-    return 0;
-}
-
 int wpsgd_softmax_loss(const void *Z, int64_t n, int64_t classes, int64_t ld, wpsgd_dtype dtype, const int64_t *labels, const float *row_weights, double scale,
-                       float *loss, void *grad, int64_t ld_grad, void *workspace, size_t workspace_bytes, void *stream)
+                       float *loss, void *grad, int64_t ld_grad, void *stream)
 {
     if (n < 0 || n > 0x7FFFFFFFLL || classes < 1 || classes > 0x7FFFFFFFLL || (dtype != WPSGD_F32 && dtype != WPSGD_BF16)) return WPSGD_INVALID_ARG;
     if (n == 0) return WPSGD_OK;
@@ -180,9 +174,6 @@ int wpsgd_softmax_loss(const void *Z, int64_t n, int64_t classes, int64_t ld, wp
     if (grad && (ld_grad < classes || (uintptr_t)grad % elem != 0)) return WPSGD_INVALID_ARG;
     if (grad == Z && ld_grad != ld) return WPSGD_INVALID_ARG;
     if (!(scale - scale == 0.0)) return WPSGD_INVALID_ARG;
-    const size_t need = wpsgd_softmax_loss_workspace(n, classes, dtype);
-    if (need && (!workspace || (uintptr_t)workspace % 256 != 0)) return WPSGD_INVALID_ARG;
-    if (workspace_bytes < need) return WPSGD_WORKSPACE_TOO_SMALL;
     const LossArgs a{Z, n, classes, ld, labels, row_weights, (float)scale, loss, grad, ld_grad};
     hipStream_t s = static_cast<hipStream_t>(stream);
     const hipError_t e = dtype == WPSGD_F32 ? launch_loss<float>(a, s) : launch_loss<uint16_t>(a, s);

@@ -57,7 +57,7 @@ def test_quantize():
 
 
 def loss(Z=GB, n=4, c=10, ld=10, dtype=api.F32, labels=GB, scale=1.0, out=GB, grad=2 * GB, ld_grad=10):
-    return api.load().wpsgd_softmax_loss(Z, n, c, ld, dtype, labels, None, scale, out, grad, ld_grad, None, 0, None)
+    return api.load().wpsgd_softmax_loss(Z, n, c, ld, dtype, labels, None, scale, out, grad, ld_grad, None)
 
 
 @pytest.mark.parametrize("change", [dict(Z=None), dict(n=-1), dict(c=0), dict(ld=9), dict(dtype=3), dict(labels=None), dict(scale=math.nan), dict(scale=math.inf),
@@ -70,7 +70,7 @@ def draw(Z=GB, n=4, c=10, ld=10, dtype=api.F32, u=GB, drawn=GB, **rule):
     r = api._CDrawRule(1.0, 0, 1.0, 0.0)
     for k, v in rule.items():
         setattr(r, k, v)
-    return api.load().wpsgd_draw_classes(Z, n, c, ld, dtype, u, ctypes.byref(r), drawn, None, None, 0, None)
+    return api.load().wpsgd_draw_classes(Z, n, c, ld, dtype, u, ctypes.byref(r), drawn, None, None)
 
 
 @pytest.mark.parametrize("change", [dict(Z=None), dict(n=-1), dict(c=0), dict(ld=9), dict(dtype=2), dict(u=None), dict(drawn=None), dict(temperature=-0.5),
@@ -82,7 +82,7 @@ def test_draw(change):
 def test_draw_limits():
     assert draw(c=(1 << 18) + 1, ld=1 << 19) == api.UNSUPPORTED
     assert draw(n=0) == loss(n=0) == api.OK
-    assert api.load().wpsgd_draw_classes(GB, 4, 10, 10, 0, GB, None, GB, None, None, 0, None) == api.INVALID_ARG
+    assert api.load().wpsgd_draw_classes(GB, 4, 10, 10, 0, GB, None, GB, None, None) == api.INVALID_ARG
 
 
 def test_tensor_lists():

@@ -187,6 +187,7 @@ def test_refusals():
     assert status(lambda: api.wpsgd_quantize(X, exps=narrow)) == api.INVALID_ARG                        # a stride that is no whole words
     other = api.wpsgd_quantize(api.Matrix(4, 100, dense=x[:, :100]))
     assert status(lambda: api.wpsgd_block_matmul(a, other)) == api.INVALID_ARG                          # different lengths
+    assert status(lambda: api.wpsgd_block_matmul(a, a, out=torch.empty(4, device="cuda").expand(4, 4))) == api.INVALID_ARG      # rows on top of each other
     with pytest.raises(AssertionError):
         api.wpsgd_block_matmul(a, a, out=torch.empty((4, 5), device="cuda"))
     with pytest.raises(AssertionError):

@@ -107,13 +107,22 @@ __global__ __launch_bounds__(64 * kRowWaves) void matmul_rows_kernel(MatmulArgs 
             if (step % per == 0) {
                 const int b0 = step / per * kHeld, n = g.blocks - b0 < kHeld ? g.blocks - b0 : kHeld;
                 if (step > 0) __syncthreads();
-                for (int item = wave; item < n * MT * 2; item += kRowWaves) {      // block, rows, half
-                    const int h = item & 1, t = (item >> 1) % MT, b = b0 + (item >> 1) / MT;
+                // items of block, rows and half, all of a wave's on their way at once
+                constexpr int kItems = kHeldBlocks * 2 / kRowWaves;
+                uint4 q[kItems];
+                uint8_t c[kItems];
+#pragma unroll
+                for (int x = 0; x < kItems; ++x) {
+                    const int item = wave + x * kRowWaves, t = (item >> 1) % MT, in = (item >> 1) / MT, at = b0 + (in < n ? in : n - 1);
                     const int64_t i = h0 + t * 16 + r < rows_few ? h0 + t * 16 + r : rows_few - 1;
-                    const uint4 q = *reinterpret_cast<const uint4 *>(few + i * ld_few + (int64_t)b * 128 + h * 64 + group * 16);
-                    const float c = power_of(few_e[i * lde_few + b]);
-                    lds.held[(item >> 1) * 4 + h * 2][lane] = widen8(q.x, q.y, c);
-                    lds.held[(item >> 1) * 4 + h * 2 + 1][lane] = widen8(q.z, q.w, c);
+                    q[x] = *reinterpret_cast<const uint4 *>(few + i * ld_few + (int64_t)at * 128 + (item & 1) * 64 + group * 16);
+                    c[x] = few_e[i * lde_few + at];
+                }
+#pragma unroll
+                for (int x = 0; x < kItems; ++x) {
+                    const int item = wave + x * kRowWaves;
+                    lds.held[(item >> 1) * 4 + (item & 1) * 2][lane] = widen8(q[x].x, q[x].y, power_of(c[x]));
+                    lds.held[(item >> 1) * 4 + (item & 1) * 2 + 1][lane] = widen8(q[x].z, q[x].w, power_of(c[x]));
                 }
                 __syncthreads();
             }

@@ -21,7 +21,7 @@ __device__ inline float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog
 
 // The row waits in registers between its statistics and its gradient, V vectors of sixteen bytes to a thread, so that it is read once; NT threads to a row, 256 / NT
 // rows to a workgroup where that is more than one.  LONG: what a row has beyond 16 NT V bytes is read again for the gradient.  Bound by memory: 8192 x 65536
-// bfloat16 reads and writes 1 GiB each.
+// bfloat16 reads and writes 1 GiB each in 385 us, 5.6 TB/s; 1023 x 32001 takes 24 us, 5.4 TB/s; 64 x 1000 fp32 3.6 us, a launch.
 template <typename T, int NT, int V, bool LONG>
 __global__ __launch_bounds__(NT < 256 ? 256 : NT) void softmax_row_kernel(LossArgs a)
 {

@@ -26,7 +26,7 @@ struct Chunk {
     int32_t dtype;
     int64_t unused;
 };
-static_assert(sizeof(Chunk) == 32, "two to a cache line quarter");
+static_assert(sizeof(Chunk) == 32, "four to a line of 128 bytes");
 
 constexpr int kAtOnce = 4;               // vectors on their way
 

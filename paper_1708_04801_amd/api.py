@@ -569,12 +569,14 @@ def wpsgd_quantize(X: Matrix, rows: Optional[torch.Tensor] = None, transpose=Fal
     r, c = (X.d, n) if transpose else (n, X.d)
     blocks = -(-c // 128)
     source = X.dense if X.dense is not None else X.vals
+    new = codes is None and exps is None
     if codes is None:
-        codes = torch.empty((r, 128 * blocks), dtype=torch.float8_e4m3fn, device=source.device)
+        codes = source.new_empty((r, 128 * blocks), dtype=torch.float8_e4m3fn)
     if exps is None:
-        exps = torch.empty((r, (blocks + 3) // 4 * 4), dtype=torch.uint8, device=source.device)
+        exps = source.new_empty((r, (blocks + 3) // 4 * 4), dtype=torch.uint8)
     out = BlockMatrix(r, c, codes, exps)
-    rc = load().wpsgd_quantize(ctypes.byref(cm), picked, n, 1 if transpose else 0, ctypes.byref(out.c_struct()), _stream_of(stream, source))
+    c_out = _CBlocks(r, c, codes.data_ptr(), 128 * blocks, exps.data_ptr(), (blocks + 3) // 4 * 4) if new else out.c_struct()
+    rc = load().wpsgd_quantize(ctypes.byref(cm), picked, n, 1 if transpose else 0, ctypes.byref(c_out), _stream_of(stream, source))
     if rc != OK:
         raise WpsgdError(rc, "wpsgd_quantize")
     return out
@@ -588,7 +590,7 @@ def wpsgd_block_matmul(A: BlockMatrix, B: BlockMatrix, out: Optional[torch.Tenso
                        workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """out[i, j] = sum_c A[i, c] B[j, c], float32 or bfloat16."""
     if out is None:
-        out = torch.empty((A.rows, B.rows), dtype=dtype, device=A.codes.device)
+        out = A.codes.new_empty((A.rows, B.rows), dtype=dtype)
     assert out.is_cuda and out.dtype in _DTYPES and out.shape == (A.rows, B.rows) and (out.numel() == 0 or out.stride(1) == 1)
     L = load()
     p, size, held = _call_workspace(workspace, L.wpsgd_block_matmul_workspace(A.rows, B.rows, A.cols), out.device, stream)
@@ -615,10 +617,10 @@ def wpsgd_softmax_loss(Z: torch.Tensor, labels: torch.Tensor, scale=1.0, row_wei
     if row_weights is not None:
         assert row_weights.is_cuda and row_weights.dtype == torch.float32 and row_weights.is_contiguous() and row_weights.numel() == n
     if loss is None:
-        loss = torch.empty(n, dtype=torch.float32, device=Z.device)
+        loss = Z.new_empty(n, dtype=torch.float32)
     assert loss.is_cuda and loss.dtype == torch.float32 and loss.is_contiguous() and loss.numel() == n
     if grad is True:
-        grad = torch.empty((n, c), dtype=Z.dtype, device=Z.device)
+        grad = Z.new_empty((n, c))
         g_ptr, g_ld = grad.data_ptr(), c
     elif grad is not False and grad is not None:
         gn, gc, g_ld = _rows_of(grad)
@@ -671,7 +673,7 @@ def wpsgd_grad_norm_workspace(tensors: TensorList) -> int:
 def _norm_call(name, tensors, args, norm, workspace, stream):
     L = load()
     if norm is None:
-        norm = torch.empty((), dtype=torch.float32, device=tensors.table.device)
+        norm = tensors.table.new_empty((), dtype=torch.float32)
     assert norm.is_cuda and norm.dtype == torch.float32 and norm.numel() == 1
     c_list = ctypes.byref(tensors.c_list)
     p, size, held = _call_workspace(workspace, L.wpsgd_grad_norm_workspace(c_list), norm.device, stream)
@@ -713,9 +715,9 @@ def wpsgd_draw_classes(Z: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=
         else:
             setattr(rule, name, v)
     if drawn is None:
-        drawn = torch.empty(n, dtype=torch.int64, device=Z.device)
+        drawn = u.new_empty(n, dtype=torch.int64)
     if probs is None:
-        probs = torch.empty(n, dtype=torch.float32, device=Z.device)
+        probs = u.new_empty(n)
     assert drawn.is_cuda and drawn.dtype == torch.int64 and drawn.is_contiguous() and drawn.numel() == n
     assert probs.is_cuda and probs.dtype == torch.float32 and probs.is_contiguous() and probs.numel() == n
     rc = load().wpsgd_draw_classes(Z.data_ptr(), n, c, ld, _DTYPES[Z.dtype], u.data_ptr(), ctypes.byref(rule), drawn.data_ptr(), probs.data_ptr(),

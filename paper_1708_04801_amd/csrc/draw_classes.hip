@@ -839,8 +839,9 @@ template <typename T>
 static hipError_t launch_draw(const DrawArgs &a, hipStream_t s)
 {
     const dim3 grid((unsigned)a.n);
-    // short rows: four waves, several workgroups to a compute unit
-    if (a.c <= 4096) hipLaunchKernelGGL((draw_row_kernel<T, 256, 2048>), grid, dim3(256), 0, s, a);
+    // short rows: four waves, whose barriers are shorter, and several workgroups to a compute unit (us a call with top_p 0.9, four waves | sixteen, bfloat16: 200 rows of
+    // 8000 16.4 | 20.8, one of 16000 17.5 | 21.4, but fp32, 200 of 16000 28.8 | 22.8, and with top 50 13.4 | 11.2)
+    if (a.c <= 8192) hipLaunchKernelGGL((draw_row_kernel<T, 256, 2048>), grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL((draw_row_kernel<T, 1024, 14336>), grid, dim3(1024), 0, s, a);
     return hipGetLastError();
 }

@@ -197,3 +197,23 @@ def test_refusals():
     drawn, _ = api.wpsgd_draw_classes(z, u + 0.9, temperature=torch.tensor([-1.0, math.nan, 1.0], device="cuda"),
                                       min_p=torch.tensor([0.0, 0.0, 7.0], device="cuda"))
     assert drawn.tolist() == [0, 0, 7]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("c", [61, 64, 65, 128, 129, 255, 257, 8192, 8193])
+def test_lists_about_as_long_as_those_compared_each_with_each(c, dtype):
+    """few classes, so that all of them are listed, and the row lengths on both sides of the number of threads' change"""
+    z = whole_scores(5, c, dtype, 3 * c)
+    g = torch.Generator().manual_seed(c)
+    for rule in (dict(top_k=50), dict(top_k=60, top_p=0.9), dict(top_k=120, top_p=0.6, min_p=0.125), dict(top_k=254), dict(top_k=40, min_p=0.5), dict(top_p=0.8)):
+        check(z, torch.rand(5, generator=g).cuda(), rule)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("c,low", [(5000, 1), (8000, 2)])
+def test_middling_rows_with_hardly_a_difference(c, low, dtype):
+    """lists without room for what reaches the top_k-th score"""
+    z = whole_scores(4, c, dtype, c + low, low=low)
+    g = torch.Generator().manual_seed(low)
+    for rule in (dict(top_k=50), dict(top_k=200, top_p=0.9), dict(top_k=2500), dict(top_p=0.5), dict(top_p=0.97), dict(min_p=0.5)):
+        check(z, torch.rand(4, generator=g).cuda(), rule)

@@ -524,6 +524,15 @@ def _stream_of(stream, t):
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _new(like, shape, dtype, stream):
+    """Memory for a result or a workspace, from the pool of the stream that the work is queued on.  (A block of the current stream's pool may still be
+    in use by work that waits there, and is handed out again as soon as its tensor goes.)"""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream_of(stream, like), like.device)):
+        return like.new_empty(shape, dtype=dtype)
+
+
 _CODES = (torch.float8_e4m3fn, torch.uint8, torch.int8)
 
 
@@ -546,14 +555,14 @@ class BlockMatrix:
         return _CBlocks(rows, cols, codes.data_ptr(), ld, exps.data_ptr(), ld_exps)
 
 
-def _call_workspace(workspace, need, device, stream):
+def _call_workspace(workspace, need, like, stream):
     """The caller's workspace, or a temporary one, as address and size, and the tensor itself: whoever calls holds on to it until the
     work is queued."""
     if workspace is None:
         if not need:
             return None, 0, None
-        workspace = _workspace(need, device, stream)
-        return workspace.data_ptr(), max(need, 256), workspace
+        workspace = _new(like, need, torch.uint8, stream)
+        return workspace.data_ptr(), need, workspace
     return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
 
 
@@ -571,9 +580,9 @@ def wpsgd_quantize(X: Matrix, rows: Optional[torch.Tensor] = None, transpose=Fal
     source = X.dense if X.dense is not None else X.vals
     new = codes is None and exps is None
     if codes is None:
-        codes = source.new_empty((r, 128 * blocks), dtype=torch.float8_e4m3fn)
+        codes = _new(source, (r, 128 * blocks), torch.float8_e4m3fn, stream)
     if exps is None:
-        exps = source.new_empty((r, (blocks + 3) // 4 * 4), dtype=torch.uint8)
+        exps = _new(source, (r, (blocks + 3) // 4 * 4), torch.uint8, stream)
     out = BlockMatrix(r, c, codes, exps)
     c_out = _CBlocks(r, c, codes.data_ptr(), 128 * blocks, exps.data_ptr(), (blocks + 3) // 4 * 4) if new else out.c_struct()
     rc = load().wpsgd_quantize(ctypes.byref(cm), picked, n, 1 if transpose else 0, ctypes.byref(c_out), _stream_of(stream, source))
@@ -590,10 +599,10 @@ def wpsgd_block_matmul(A: BlockMatrix, B: BlockMatrix, out: Optional[torch.Tenso
                        workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """out[i, j] = sum_c A[i, c] B[j, c], float32 or bfloat16."""
     if out is None:
-        out = A.codes.new_empty((A.rows, B.rows), dtype=dtype)
+        out = _new(A.codes, (A.rows, B.rows), dtype, stream)
     assert out.is_cuda and out.dtype in _DTYPES and out.shape == (A.rows, B.rows) and (out.numel() == 0 or out.stride(1) == 1)
     L = load()
-    p, size, held = _call_workspace(workspace, L.wpsgd_block_matmul_workspace(A.rows, B.rows, A.cols), out.device, stream)
+    p, size, held = _call_workspace(workspace, L.wpsgd_block_matmul_workspace(A.rows, B.rows, A.cols), out, stream)
     rc = L.wpsgd_block_matmul(ctypes.byref(A.c_struct()), ctypes.byref(B.c_struct()), out.data_ptr(), out.stride(0) if A.rows > 1 else max(out.stride(0), B.rows),
                               _DTYPES[out.dtype], p, size, _stream_of(stream, out))
     if rc != OK:
@@ -617,10 +626,10 @@ def wpsgd_softmax_loss(Z: torch.Tensor, labels: torch.Tensor, scale=1.0, row_wei
     if row_weights is not None:
         assert row_weights.is_cuda and row_weights.dtype == torch.float32 and row_weights.is_contiguous() and row_weights.numel() == n
     if loss is None:
-        loss = Z.new_empty(n, dtype=torch.float32)
+        loss = _new(Z, n, torch.float32, stream)
     assert loss.is_cuda and loss.dtype == torch.float32 and loss.is_contiguous() and loss.numel() == n
     if grad is True:
-        grad = Z.new_empty((n, c))
+        grad = _new(Z, (n, c), Z.dtype, stream)
         g_ptr, g_ld = grad.data_ptr(), c
     elif grad is not False and grad is not None:
         gn, gc, g_ld = _rows_of(grad)
@@ -644,7 +653,8 @@ class TensorList:
 
 
 def wpsgd_tensor_list(grads, weights=None, stream=None) -> TensorList:
-    """Gradients (float32 or bfloat16) and, for steps, the weights (float32) of the same sizes; all contiguous, on one GPU."""
+    """Gradients (float32 or bfloat16) and, for steps, the weights (float32) of the same sizes; all contiguous, on one GPU.
+    The list is ready when the stream has come to it: a call on another stream has to wait, as for any tensor."""
     grads = list(grads)
     weights = list(weights) if weights is not None else None
     assert weights is None or len(weights) == len(grads)
@@ -658,7 +668,7 @@ def wpsgd_tensor_list(grads, weights=None, stream=None) -> TensorList:
         items[i] = _CTensor(g.data_ptr(), w.data_ptr() if w is not None else None, g.numel(), _DTYPES[g.dtype])
     L = load()
     need = L.wpsgd_tensor_list_bytes(items, len(grads))
-    table = _workspace(need, device, stream)
+    table = _new(grads[0] if grads else torch.empty(0, device=device), need, torch.uint8, stream)
     c_list = _CTensorList()
     rc = L.wpsgd_tensor_list_make(items, len(grads), table.data_ptr(), table.numel(), ctypes.byref(c_list), _stream(stream))
     if rc != OK:
@@ -673,10 +683,10 @@ def wpsgd_grad_norm_workspace(tensors: TensorList) -> int:
 def _norm_call(name, tensors, args, norm, workspace, stream):
     L = load()
     if norm is None:
-        norm = tensors.table.new_empty((), dtype=torch.float32)
+        norm = _new(tensors.table, (), torch.float32, stream)
     assert norm.is_cuda and norm.dtype == torch.float32 and norm.numel() == 1
     c_list = ctypes.byref(tensors.c_list)
-    p, size, held = _call_workspace(workspace, L.wpsgd_grad_norm_workspace(c_list), norm.device, stream)
+    p, size, held = _call_workspace(workspace, L.wpsgd_grad_norm_workspace(c_list), norm, stream)
     rc = getattr(L, name)(c_list, *args, norm.data_ptr(), p, size, _stream_of(stream, norm))
     if rc != OK:
         raise WpsgdError(rc, name)
@@ -715,9 +725,9 @@ def wpsgd_draw_classes(Z: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=
         else:
             setattr(rule, name, v)
     if drawn is None:
-        drawn = u.new_empty(n, dtype=torch.int64)
+        drawn = _new(u, n, torch.int64, stream)
     if probs is None:
-        probs = u.new_empty(n)
+        probs = _new(u, n, torch.float32, stream)
     assert drawn.is_cuda and drawn.dtype == torch.int64 and drawn.is_contiguous() and drawn.numel() == n
     assert probs.is_cuda and probs.dtype == torch.float32 and probs.is_contiguous() and probs.numel() == n
     rc = load().wpsgd_draw_classes(Z.data_ptr(), n, c, ld, _DTYPES[Z.dtype], u.data_ptr(), ctypes.byref(rule), drawn.data_ptr(), probs.data_ptr(),

@@ -102,3 +102,23 @@ def test_the_workers_example():
     assert all(v < start for v in workers) and average < 1.01 * sum(x * v for x, v in zip(a, workers)) and average < start
     assert answers.shape == labels.shape == (2048, 2) and bool(((answers >= 0) & (answers < 300)).all())
     assert float((answers == labels).double().mean()) > 1 / 300 + 5 * math.sqrt(1 / 300 / answers.numel())      # more often than by chance
+
+
+def test_results_for_a_named_stream_are_not_memory_that_the_current_one_still_writes():
+    """work that waits on the current stream writes to blocks that have been given back; calls that name another stream run meanwhile"""
+    s = Step(seed=2)
+    want = s.result(s())
+    sizes = {t.numel() * t.element_size() for t in want} | {8192, 256, 512} | {t.codes.numel() for t in s.keep if isinstance(t, api.BlockMatrix)} | \
+        {t.exps.numel() for t in s.keep if isinstance(t, api.BlockMatrix)} | {t.numel() * t.element_size() for t in s.keep if isinstance(t, torch.Tensor)}
+    s.W.copy_(s.W0)
+    s.keep = None
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    torch.cuda._sleep(100_000_000)                    # some tens of milliseconds
+    held = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sorted(sizes) for _ in range(8)]
+    for t in held:
+        t.fill_(0x5A)
+    del held, t
+    out = s(stream=stream)
+    stream.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, s.result(out)))

@@ -52,12 +52,18 @@ __device__ inline U dpp_whole(U v)
     else return (U)(uint32_t)dpp_move_bits<CTRL, ROW_MASK>((int)(uint32_t)(v >> 32)) << 32 | (uint32_t)dpp_move_bits<CTRL, ROW_MASK>((int)(uint32_t)v);
 }
 template <typename U>
-__device__ inline U up_to_lane(U v)                // with this lane's own
+__device__ inline U up_to_lane_of_row(U v)         // with this lane's own; rows of sixteen lanes
 {
     v += dpp_whole<0x111, 0xF>(v);                 // row_shr 1, 2, 4, 8
     v += dpp_whole<0x112, 0xF>(v);
     v += dpp_whole<0x114, 0xF>(v);
     v += dpp_whole<0x118, 0xF>(v);
+    return v;
+}
+template <typename U>
+__device__ inline U up_to_lane(U v)
+{
+    v = up_to_lane_of_row(v);
     v += dpp_whole<0x142, 0xA>(v);                 // lane 15 of a row to the next row: rows 1 and 3
     v += dpp_whole<0x143, 0xC>(v);                 // lane 31 to rows 2 and 3
     return v;
@@ -66,6 +72,21 @@ __device__ inline uint32_t of_lane(uint32_t v, int j) { return (uint32_t)__built
 __device__ inline uint64_t of_lane(uint64_t v, int j) { return (uint64_t)of_lane((uint32_t)(v >> 32), j) << 32 | of_lane((uint32_t)v, j); }
 template <typename U>
 __device__ inline U wave_total(U v) { return of_lane(up_to_lane(v), kWave - 1); }
+__device__ inline uint32_t wave_or(uint32_t v)
+{
+    v |= dpp_whole<0xB1, 0xF>(v);                  // lanes that differ in bits 0, 1, 2, 3: all of a row
+    v |= dpp_whole<0x4E, 0xF>(v);
+    v |= dpp_whole<0x141, 0xF>(v);
+    v |= dpp_whole<0x140, 0xF>(v);
+    return of_lane(v, 0) | of_lane(v, 16) | of_lane(v, 32) | of_lane(v, 48);
+}
+__device__ inline float row_max(float v)           // of sixteen lanes
+{
+    v = fmaxf(v, dpp_move<0xB1, 0xF>(v));
+    v = fmaxf(v, dpp_move<0x4E, 0xF>(v));
+    v = fmaxf(v, dpp_move<0x141, 0xF>(v));
+    return fmaxf(v, dpp_move<0x140, 0xF>(v));
+}
 
 // ---- a row in a workgroup ----
 // A wave owns a run of classes, in vectors of sixteen bytes to a lane; kRun vectors of a wave are a "segment".  The row is read again for each step, from the caches:
@@ -80,10 +101,10 @@ __device__ inline U wave_total(U v) { return of_lane(up_to_lane(v), kWave - 1); 
 //      corrects the sample for another try; after four the end is looked for among all classes digit by digit, and a pass adds up the segments;
 //   4. the draw: the segment in which the target lies, then the class.
 //
-// (us a call, 256 rows of 131072 bfloat16: all kept 36, top 50 35, top_p 0.9 64; 512 threads with registers to spare 34, 36 and 58, but one row of 32000 with
-// top 50 and top_p 0.95 takes 16.4 instead of 13.8, and half as large a sample misses the run's end more often.)
-// 256 rows of 131072 bfloat16 scores, a row to a compute unit: 14 us for the first step, which is bound by memory, 8 to 20 for a pass that forms weights
-// (17 instructions an element, four of them the power of two).
+// (us a call, 256 rows of 131072 bfloat16: all kept 36, top 50 33, top_p 0.9 61; 512 threads with registers to spare 34, 36 and 58, but one row of 32000 with
+// top 50 and top_p 0.95 took a fifth longer, and half as large a sample misses the run's end more often.)
+// 256 rows of 131072 bfloat16 scores, a row to a compute unit: 10 us for the first step, which is bound by memory, 15 for a pass that forms weights
+// (17 instructions an element, four of them the power of two), 22 for one that also lists; the sample 9, the run's end in a list of thousands 10.
 constexpr int kBins = 1024, kCopies = 2;
 constexpr int kMostClasses = 1 << 18;
 
@@ -107,8 +128,9 @@ struct Row {
         unsigned long long segment[kSegments];
         float tops[2 * kWaves];
         uint32_t ties[kSegments];
-        uint64_t found[2];
-        uint64_t sums[kWaves];
+        uint64_t found[3];
+        uint64_t sums[3][16];                      // of the waves, as many as there are
+        uint32_t bits[16];
         uint32_t count;
     };
     Shared *sh;
@@ -167,16 +189,39 @@ struct Row {
     {
         __syncthreads();
     }
+    // What the waves have left, a lane of each row of sixteen to a wave: a read for all of them, where a read each is sixteen to every wave.
+    __device__ __forceinline__ uint64_t waves_total(int which) const
+    {
+        const int w = t & 15;
+        return of_lane(up_to_lane_of_row(w < kWaves ? sh->sums[which][w] : (uint64_t)0), 15);
+    }
     __device__ __forceinline__ uint64_t group_sum(uint64_t v)
     {
         v = wave_total(v);
         barrier();
-        if ((t & 63) == 0) sh->sums[t >> 6] = v;
+        if ((t & 63) == 0) sh->sums[0][t >> 6] = v;
         barrier();
-        uint64_t s = 0;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) s += sh->sums[w];
-        return s;
+        return waves_total(0);
+    }
+    // three sums and the bits of a fourth value at once
+    __device__ __forceinline__ void group_sums(uint64_t &a, uint64_t &b, uint64_t &c, uint32_t &bits)
+    {
+        a = wave_total(a);
+        b = wave_total(b);
+        c = wave_total(c);
+        bits = wave_or(bits);
+        barrier();
+        if ((t & 63) == 0) {
+            sh->sums[0][t >> 6] = a;
+            sh->sums[1][t >> 6] = b;
+            sh->sums[2][t >> 6] = c;
+            sh->bits[t >> 6] = bits;
+        }
+        barrier();
+        a = waves_total(0);
+        b = waves_total(1);
+        c = waves_total(2);
+        bits = wave_or((t & 15) < kWaves ? sh->bits[t & 15] : 0);
     }
     // Where in descending order of a 32-bit key the sum of the values reaches goal: the key, and the sum in front of it.  walk(f) calls f(key, value) for
     // the classes of this thread that take part, whose keys lie between lo and hi; digits that these share are not looked at.  BITS: how many of the key's upper bits may differ.
@@ -229,29 +274,17 @@ struct Row {
     {
         for (uint32_t i = t; i < sh->count; i += NT) f((uint32_t)(sh->list[i] >> 32), (uint32_t)sh->list[i]);
     }
-    // the least and the largest key in the list
+    // two keys that differ where any in the list do (one at least)
     __device__ __forceinline__ void list_range(uint32_t &lo, uint32_t &hi)
     {
-        lo = 0xFFFFFFFFu;
-        hi = 0;
-        each_listed([&](uint32_t key, uint32_t) {
-            lo = key < lo ? key : lo;
-            hi = key > hi ? key : hi;
-        });
-        for (int d = 1; d < 64; d *= 2) {
-            const uint32_t a = __shfl_xor(lo, d), b = __shfl_xor(hi, d);
-            lo = a < lo ? a : lo;
-            hi = b > hi ? b : hi;
-        }
         barrier();
-        if ((t & 63) == 0) sh->sums[t >> 6] = (uint64_t)hi << 32 | lo;
+        lo = (uint32_t)(sh->list[0] >> 32);
+        uint32_t differ = 0;
+        each_listed([&](uint32_t key, uint32_t) { differ |= key ^ lo; });
+        differ = wave_or(differ);
+        if ((t & 63) == 0) sh->bits[t >> 6] = differ;
         barrier();
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const uint32_t a = (uint32_t)sh->sums[w], b = (uint32_t)(sh->sums[w] >> 32);
-            lo = a < lo ? a : lo;
-            hi = b > hi ? b : hi;
-        }
+        hi = lo ^ wave_or((t & 15) < kWaves ? sh->bits[t & 15] : 0);
     }
     // the bin of a score: how far it lies below the largest, in powers of two times scale
     __device__ __forceinline__ int bin_of_powers(float z) const
@@ -281,36 +314,35 @@ struct Row {
             mine += h[j];
         }
         const uint64_t in = up_to_lane(mine);
-        if ((t & 63) == 63) sh->sums[t >> 6] = in;
+        if ((t & 63) == 63) sh->sums[0][t >> 6] = in;
         barrier();
-        uint64_t before = in - mine, all = 0;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const uint64_t s = sh->sums[w];
-            before += w < (t >> 6) ? s : 0;
-            all += s;
-        }
-        front[0] = before;
+        const int w = t & 15, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+        const uint64_t waves = up_to_lane_of_row(w < kWaves ? sh->sums[0][w] : (uint64_t)0), all = of_lane(waves, 15);
+        front[0] = in - mine + (wave > 0 ? of_lane(waves, wave - 1) : 0);
 #pragma unroll
         for (int j = 0; j < kMine; ++j) front[j + 1] = front[j] + h[j];
         return all;
     }
-    // the first bin at which the sum reaches goal (more than 0, at most the sum of all), and the sum in front of it
-    __device__ __forceinline__ int find_bin(const uint64_t (&front)[kMine + 1], uint64_t goal, uint64_t &before)
+    // the first bin at which the sum reaches goal (more than 0, at most the sum of all), and the sum in front of it; the same of a second goal, if that is more than 0
+    __device__ __forceinline__ int find_bin(const uint64_t (&front)[kMine + 1], uint64_t goal, uint64_t &before, uint64_t goal2 = 0, int *bin2 = nullptr)
     {
         barrier();
 #pragma unroll
-        for (int j = 0; j < kMine; ++j)
+        for (int j = 0; j < kMine; ++j) {
             if (front[j] < goal && goal <= front[j + 1]) {
                 sh->found[0] = (uint64_t)(t * kMine + j);
                 sh->found[1] = front[j];
             }
+            if (front[j] < goal2 && goal2 <= front[j + 1]) sh->found[2] = (uint64_t)(t * kMine + j);
+        }
         barrier();
         before = sh->found[1];
+        if (bin2) *bin2 = (int)sh->found[2];
         return (int)sh->found[0];
     }
-    // Appends a lane's classes to the list: bit j of which for class i(j).  One addition to its length for the wave.
-    template <typename I>
+    // Appends a lane's classes to the list: bit j of which for class i(j).  One addition to its length for the wave.  KEYS: with the scores' keys, four looked up at
+    // a time, which pays for a list of thousands: afterwards they would be one more way through the row.
+    template <bool KEYS = false, typename I>
     __device__ __forceinline__ void append(uint32_t which, I &&i)
     {
         const uint32_t n = (uint32_t)__popc(which), n_in = up_to_lane(n), all = of_lane(n_in, kWave - 1);
@@ -319,11 +351,37 @@ struct Row {
         if ((t & 63) == 0) at = atomicAdd(&sh->count, all);
         at = of_lane(at, 0) + n_in - n;
         while (which) {
-            const int j = __ffs(which) - 1;
-            which &= which - 1;
-            const int c = i(j);
-            if (at < CAP) sh->list[at] = (uint64_t)key_of(Elem<T>::load(z + c) + 0.0f) << 32 | (uint32_t)c;
-            ++at;
+            constexpr int kMany = KEYS ? 4 : 1;
+            int c[kMany];
+            uint64_t o[kMany];
+            const int n = __popc(which);
+#pragma unroll
+            for (int j = 0; j < kMany; ++j) {
+                c[j] = which ? i(__ffs(which) - 1) : c[0];
+                which &= which - 1;
+            }
+#pragma unroll
+            for (int j = 0; j < kMany; ++j) o[j] = KEYS ? entry_of((uint32_t)c[j]) : (uint64_t)(uint32_t)c[j];
+#pragma unroll
+            for (int j = 0; j < kMany; ++j)
+                if (j < n && at + j < CAP) sh->list[at + j] = o[j];
+            at += kMany;
+        }
+    }
+    __device__ __forceinline__ uint64_t entry_of(uint32_t i) const { return (uint64_t)key_of(Elem<T>::load(z + i) + 0.0f) << 32 | i; }
+    // The keys beside the classes of a list that has room, behind a barrier after the last append: four of a thread's on their way at once, and a thread's own are those
+    // that it walks in each_listed.  (For a list of tens: looked up as they are appended, a wave waits for each.)
+    __device__ __forceinline__ void fill_keys()
+    {
+        constexpr int kMany = 4;
+        const uint32_t n = sh->count;
+        for (uint32_t i0 = t; i0 < n; i0 += NT * kMany) {
+            uint64_t o[kMany];
+#pragma unroll
+            for (int j = 0; j < kMany; ++j) o[j] = entry_of((uint32_t)sh->list[i0 + j * NT < n ? i0 + j * NT : i0]);
+#pragma unroll
+            for (int j = 0; j < kMany; ++j)
+                if (i0 + j * NT < n) sh->list[i0 + j * NT] = o[j];
         }
     }
 };
@@ -367,19 +425,15 @@ __global__ __launch_bounds__(NT) void draw_row_kernel(DrawArgs a)
         for (int j = 0; j < E; ++j) own = fmaxf(own, Elem<T>::get(q.w, j));
     });
     {
-        const float m = wave_max(own), n = -wave_max(own > -kInf ? -own : -kInf);
+        const float m = wave_max(own), n = wave_max(own > -kInf ? -own : -kInf);
         if (lane == 0) {
             sh.tops[wave] = m;
             sh.tops[R::kWaves + wave] = n;
         }
     }
     __syncthreads();
-    float top = sh.tops[0], least = sh.tops[R::kWaves];
-#pragma unroll
-    for (int w = 1; w < NT / 64; ++w) {
-        top = fmaxf(top, sh.tops[w]);
-        least = fminf(least, sh.tops[R::kWaves + w]);
-    }
+    float top = row_max(sh.tops[t % R::kWaves]);
+    const float least = -row_max(sh.tops[R::kWaves + t % R::kWaves]);
     __syncthreads();
     top += 0.0f;
     auto answer = [&](int64_t which, float p) {
@@ -450,13 +504,11 @@ __global__ __launch_bounds__(NT) void draw_row_kernel(DrawArgs a)
                 const int bin = row.find_bin(fronts, (uint64_t)top_k, front);
                 reach = some && row.bin_of(own) <= bin ? own : kInf;
             }
-            reach = -wave_max(-reach);
+            reach = wave_max(-reach);
             __syncthreads();
             if (lane == 0) sh.tops[wave] = reach;
             __syncthreads();
-            reach = sh.tops[0];
-#pragma unroll
-            for (int w = 1; w < NT / 64; ++w) reach = fminf(reach, sh.tops[w]);
+            reach = -row_max(sh.tops[t % R::kWaves]);
             row.each_vector([&](int v, const Bytes16 &q) {
                 float most = Elem<T>::get(q.w, 0);
 #pragma unroll
@@ -480,8 +532,10 @@ __global__ __launch_bounds__(NT) void draw_row_kernel(DrawArgs a)
             // 256 threads take 23 us a call for a list of 200 bfloat16 scores, and 10 by digits.  Its place in order and the weight in front of it say whether it is
             // kept, the kept weight in front of it by index whether it is drawn.
             const int n = (int)sh.count, shift = n <= 64 ? 6 : n <= 128 ? 7 : 8, parts = NT >> shift, mine = t & ((1 << shift) - 1), part = t >> shift;
-            const uint64_t me = mine < n ? sh.list[mine] : 0;
-            if (t < 4) sh.list[n + t] = 0xFFFFFFFFull;                   // in front of nothing, in either order
+            const uint64_t me = mine < n ? row.entry_of((uint32_t)sh.list[mine]) : 0;
+            __syncthreads();
+            if (t < n) sh.list[t] = me;
+            else if (t < n + 4) sh.list[t] = 0xFFFFFFFFull;              // in front of nothing, in either order
             const uint64_t order = me ^ 0xFFFFFFFFull;                   // larger: in front
             if (t < R::kShort) {
                 const uint32_t q = t < n ? weigh(of_key((uint32_t)(me >> 32))) : 0u;
@@ -533,6 +587,7 @@ __global__ __launch_bounds__(NT) void draw_row_kernel(DrawArgs a)
             if (part == 0 && kept && before <= target && target < before + q) answer((int64_t)(uint32_t)me, (float)((double)q / (double)total));
             return;
         }
+        if (listed) row.fill_keys();
         if (cut_k) {
             uint64_t before = 0;
             const uint64_t k = (uint64_t)top_k;
@@ -560,7 +615,7 @@ __global__ __launch_bounds__(NT) void draw_row_kernel(DrawArgs a)
                             const float x = Elem<T>::get(q.w, j);
                             which |= x > -kInf && row.bin_of(x) == bin ? 1u << j : 0u;
                         }
-                        row.append(which, [&](int j) { return row.class_of(v) + j; });
+                        row.template append<true>(which, [&](int j) { return row.class_of(v) + j; });
                     });
                     __syncthreads();
                     uint64_t in = 0;
@@ -635,8 +690,8 @@ __global__ __launch_bounds__(NT) void draw_row_kernel(DrawArgs a)
     }
 
     // The kept weight of each segment, and its ties.  BETWEEN: scores over the floor count where they are less than `sure` powers of two below the largest; down
-    // to `maybe` they go to the list, and the weight of all that do not count is returned (each thread's).
-    auto add_segments = [&](auto between, float sure, float maybe) -> uint64_t {
+    // to `maybe` they go to the list, and each thread's weight of what counts is added to `counted`, that of all others returned.
+    auto add_segments = [&](auto between, float sure, float maybe, uint64_t &counted) -> uint64_t {
         constexpr bool BETWEEN = decltype(between)::value;
         const bool tied = !BETWEEN && ties > 0;
         uint64_t rest = 0;
@@ -668,7 +723,8 @@ __global__ __launch_bounds__(NT) void draw_row_kernel(DrawArgs a)
             }
             if constexpr (BETWEEN) {
                 rest -= mine;
-                row.append(listed_ones, [&](int j) { return row.class_of(g * R::kRun + j / E) + j % E; });
+                counted += mine;
+                row.template append<true>(listed_ones, [&](int j) { return row.class_of(g * R::kRun + j / E) + j % E; });
             }
             mine = wave_total(mine);
             if (tied) equal = wave_total(equal);
@@ -702,41 +758,51 @@ __global__ __launch_bounds__(NT) void draw_row_kernel(DrawArgs a)
         double goal = (double)top_p * (double)sample, margin = kMargin * fmax((double)top_p * (1.0 - (double)top_p), 0.006) * (double)sample;     // in the sample's weight
         uint64_t need = 0, over = 0, rest = 0, before = 0;
         float end = floor;
+        // min_p or top_k may say that few classes are kept at all (half the sample's weight is about the row's): a sample says little of their order then, and all of them
+        // have room in the list
+        double most = low > 0.0f ? 0.5 * (double)sample / ((double)low * (double)kOne) : (double)kMostClasses;
+        if (cut_k && (double)top_k < most) most = (double)top_k;
+        bool whole = most < 0.7 * CAP;
         bool found = false;
+        uint32_t first = 0, differ = 0;            // a key of the list, and the bits in which any differ from it
         for (int tries = 0; tries < 4 && !found && sample > 0; ++tries) {
             uint64_t sampled = 0;                  // the sample's weight over `sure`
             float sure = 1.0f, maybe = -kInf;      // (even the largest may be the last)
-            __syncthreads();
-            if (goal - margin > 1.0) {
-                const double from = goal - margin < (double)sample ? goal - margin : (double)sample;
-                sure = (float)row.find_bin(fronts, (uint64_t)from, sampled) / -row.scale;
-            }
-            if (goal + margin < (double)sample) {
-                const int last = row.find_bin(fronts, (uint64_t)(goal + margin > 1.0 ? goal + margin : 1.0), before);
-                if (last < kBins - 1) maybe = (float)(last + 1) / -row.scale;
-            }
+            const uint64_t from = !whole && goal - margin > 1.0 ? (uint64_t)(goal - margin < (double)sample ? goal - margin : (double)sample) : 0;
+            const uint64_t to = !whole && goal + margin < (double)sample ? (uint64_t)(goal + margin > 1.0 ? goal + margin : 1.0) : 0;
+            int last = kBins - 1;
+            const int bin = row.find_bin(fronts, from, sampled, to, &last);
+            if (from > 0) sure = (float)bin / -row.scale;
+            else sampled = 0;
+            if (to > 0 && last < kBins - 1) maybe = (float)(last + 1) / -row.scale;
             if (t == 0) sh.count = 0;
             __syncthreads();
-            rest = row.group_sum(add_segments(std::true_type{}, sure, maybe));
-            uint64_t mine = 0;
-            for (int i = t; i < segments; i += NT) mine += sh.segment[i];
-            over = row.group_sum(mine);
+            over = 0;
+            rest = add_segments(std::true_type{}, sure, maybe, over);
+            __syncthreads();
+            const bool room = sh.count <= CAP;
+            uint64_t list = 0;
+            differ = 0;
+            first = 0;
+            if (room && sh.count > 0) {
+                first = (uint32_t)(sh.list[0] >> 32);
+                row.each_listed([&](uint32_t key, uint32_t) {
+                    list += weigh(of_key(key));
+                    differ |= key ^ first;
+                });
+            }
+            row.group_sums(rest, over, list, differ);
             need = need_of(over + rest + ties * q_floor);
             if (need > over + rest) break;         // among the ties that top_k has left
-            mine = 0;
-            const bool room = sh.count <= CAP;
-            if (room) row.each_listed([&](uint32_t key, uint32_t) { mine += weigh(of_key(key)); });
-            const uint64_t list = row.group_sum(mine);
             found = room && need > over && need <= over + list;
             // what has been added up says what the sample's weights are worth on this side of `sure`
             if (need > over) goal = (double)sampled + (double)(need - over) * ((double)(sample - sampled) / (double)rest);
             else goal = (double)sampled * ((double)need / (double)over);
-            margin *= room ? 0.5 : 0.2;
+            if (!whole) margin *= room ? 0.5 : 0.2;
+            whole = false;
         }
-        uint32_t lo, hi;
         if (found) {
-            row.list_range(lo, hi);
-            end = of_key(row.template select<R::kKeyBits>(walk_list([&](uint32_t key) -> uint64_t { return weigh(of_key(key)); }), need - over, before, lo, hi));
+            end = of_key(row.template select<R::kKeyBits>(walk_list([&](uint32_t key) -> uint64_t { return weigh(of_key(key)); }), need - over, before, first, first ^ differ));
             before += over;
             const uint32_t end_key = key_of(end + 0.0f);
             row.each_listed([&](uint32_t key, uint32_t i) {
@@ -764,7 +830,8 @@ __global__ __launch_bounds__(NT) void draw_row_kernel(DrawArgs a)
     }
     if (!added) {
         __syncthreads();
-        add_segments(std::false_type{}, 0.0f, 0.0f);
+        uint64_t unused = 0;
+        add_segments(std::false_type{}, 0.0f, 0.0f, unused);
     }
     __syncthreads();
     const bool tied = ties > 0;
@@ -791,7 +858,7 @@ __global__ __launch_bounds__(NT) void draw_row_kernel(DrawArgs a)
                 sh.found[0] = target - front;
                 sh.found[1] = n_front;
                 sh.count = (uint32_t)i;
-                sh.sums[0] = total;
+                sh.sums[0][0] = total;
             }
             seen += of_lane(w_in, 63);
             used += of_lane(n_in, 63);
@@ -801,7 +868,7 @@ __global__ __launch_bounds__(NT) void draw_row_kernel(DrawArgs a)
     __syncthreads();
     const int segment = (int)sh.count;
     if (segment / row.runs() != wave) return;
-    total = sh.sums[0];
+    total = sh.sums[0][0];
     uint64_t inside = sh.found[0], rank0 = sh.found[1];
     for (int v = (segment % row.runs()) * R::kRun; v < (segment % row.runs() + 1) * R::kRun; ++v) {
         const Bytes16 q = row.fetch(v);

@@ -217,3 +217,31 @@ def test_middling_rows_with_hardly_a_difference(c, low, dtype):
     g = torch.Generator().manual_seed(low)
     for rule in (dict(top_k=50), dict(top_k=200, top_p=0.9), dict(top_k=2500), dict(top_p=0.5), dict(top_p=0.97), dict(min_p=0.5)):
         check(z, torch.rand(4, generator=g).cuda(), rule)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("c", [6000, 15000, 26246, 131072])
+def test_many_kept_of_rows_in_which_few_threads_have_scores(c, dtype):
+    """top_k near the number of threads: scores in a corner of the row, in few places all over it, and everywhere"""
+    z = whole_scores(4, c, dtype, c)
+    z[0, 1500:] = -INF
+    z[1, :c - 1200] = -INF
+    keep = torch.zeros(c, dtype=torch.bool, device="cuda")
+    keep[::37] = True
+    z[2, ~keep] = -INF
+    g = torch.Generator().manual_seed(c)
+    for rule in (dict(top_k=250), dict(top_k=1000), dict(top_k=1024, top_p=0.9), dict(top_k=1000, min_p=0.125, top_p=0.5)):
+        check(z, torch.rand(4, generator=g).cuda(), rule)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("c", [700, 8192, 30000, 131072])
+def test_min_p_that_keeps_few_or_seems_to(c, dtype):
+    """rows whose kept classes have room in a list, and rows of equal scores, of which a sample sees next to nothing"""
+    z = whole_scores(4, c, dtype, c + 1)
+    z[2] = -2.0
+    z[3] = -5.0
+    z[3, ::2] = -4.0
+    g = torch.Generator().manual_seed(c)
+    for rule in (dict(min_p=2.0 ** -6, top_p=0.9), dict(min_p=0.25, top_p=0.5), dict(min_p=2.0 ** -20, top_p=0.95), dict(top_k=2000, top_p=0.7), dict(min_p=1.0, top_p=0.99)):
+        check(z, torch.rand(4, generator=g).cuda(), rule)

@@ -48,8 +48,8 @@ __device__ inline void store4(uint16_t *p, const f32x4 &v)
 // Few rows against many.  The one operand's rows (the class vectors of a serving call) are read once, straight from memory into the matrix instructions, sixteen
 // rows times NT to a wave; the other's 16 MT rows lie in LDS as bfloat16 fragments, a few blocks of the sum at a time (asked for by each wave
 // they are a trip to the L2 a block: 16 x 65536 x 4096 79 us, 64 x 65536 x 4096 138).  kRowWaves waves to a workgroup: `along` of them share the blocks of the
-// sum in turn and add up through LDS, in their order, the others take the next rows.  Bound by memory: 16 x 65536 x 4096 reads 270 MB in 64 us, 4.2 TB/s; 1 x 4096 x
-// 4096, 17 MB in 8.9 us, is a start and a few trips.
+// sum in turn and add up through LDS, in their order, the others take the next rows.  Bound by memory: 16 x 65536 x 4096 reads 270 MB in 62 to 64 us, 4.2 TB/s and more; 1 x 4096 x
+// 4096, 17 MB in 8.6 us, is a start and a few trips.
 // `turned`: the many rows are A's (results of a lane lie below each other), else B's (beside each other).
 constexpr int kRowWaves = 8;
 constexpr int kHeldBlocks = 16;                                       // of sixteen rows: 64 KiB
@@ -330,7 +330,7 @@ __device__ inline uint32_t lds_address(const void *p) { return (uint32_t)(size_t
 // Sums of fp32 accuracy (see the top).  A block is taken in four parts of 32: a wave holds B's part as bfloat16 and takes A's 32 rows in turn, a row
 // being TN x 2 instructions; the next row's codes are on their way and the one before them is widened meanwhile.  B's next part is widened as the last row's products release
 // its registers.  The barrier stands in front of the second to last row of a block: everything of it has been read, the next block is there, and the loads
-// of the one behind that leave, a few to a row.  Bound by the matrix instructions, busy for 74 % of the cycles, and the card's power: 16384 x 4096 x 8192 765 to 790 us,
+// of the one behind that leave, a few to a row.  Bound by the matrix instructions, busy for 74 % of the cycles, and the card's power: 16384 x 4096 x 8192 750 to 790 us,
 // 1.4 PFLOP/s, where the library's bfloat16 product, which need not widen anything, takes 809.
 template <int TM, int TN, typename TO>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM * TN > 8 ? 1 : 2, TM * TN > 8 ? 1 : 2))) void matmul_tile_kernel(MatmulArgs g)
@@ -454,7 +454,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM * TN > 8
 // row's products release its registers.  LDS holds two blocks of B and five half blocks of A (rows 0 and 1, or 2 and 3, of both wave rows): B's room is free
 // once every wave has it in registers, in front of row 1, so that loads have two blocks (A) or one and a half (B) to arrive: with two whole blocks in LDS,
 // 2.0 instead of 2.6 PFLOP/s (a product whose loads are left out: 2.6).
-// Bound by the card's power: matrix instructions are busy for 67 to 77 % of the cycles and the clock falls to 1.7 GHz (8192 x 65536 x 4096 1.8 ms, 2.4 PFLOP/s).
+// Bound by the card's power: matrix instructions are busy for 67 to 77 % of the cycles and the clock falls to 1.7 GHz (8192 x 65536 x 4096 1.7 to 1.8 ms, 2.4 to 2.6 PFLOP/s, by the card).
 // Barriers stand in front of rows 1 and 3; loads complete in order, so a count of those that may still be on their way says which have come.
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void matmul_fast_kernel(MatmulArgs g)
 {

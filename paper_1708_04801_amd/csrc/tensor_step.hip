@@ -13,8 +13,8 @@
 
 namespace wpsgd {
 
-// Elements of a chunk.  A small model in small chunks, so that it spreads over the chip (3M elements: 16384 to a chunk 5.0 us for the norm and 8.8 for the step,
-// 2048 to a chunk 3.4 and 4.4); a large one in large ones, of which a workgroup has many and asks for several vectors at a time.
+// Elements of a chunk.  A small model in small chunks, so that it spreads over the chip (3M elements: the norm 7.0 us with
+// 16384 to a chunk, 4.7 with 2048; the step 9.3 with either); a large one in large ones, of which a workgroup has many and asks for several vectors at a time.
 constexpr int kLargeChunk = 16384, kSmallChunk = 2048;
 constexpr int64_t kSmallModel = 8 << 20;
 constexpr int kNormGroups = 1024;        // partial sums at most, one per workgroup

@@ -304,7 +304,8 @@ typedef struct wpsgd_blocks {
     void *codes;               /* DEVICE, one byte each, 16-byte aligned                                  */
     int64_t ld;                /* row stride in bytes, a multiple of 16, >= 128*ceil(cols/128)            */
     void *exps;                /* DEVICE, one byte (1 .. 254) for each block, 4-byte aligned              */
-    int64_t ld_exps;           /* row stride in bytes, a multiple of 4, >= ceil(cols/128)                 */
+    int64_t ld_exps;           /* row stride in bytes, a multiple of 4, >= ceil(cols/128); products read whole
+                                  words of each row, the last one's too                                   */
 } wpsgd_blocks;
 
 /* Rows of the data set X (dense; CSR: UNSUPPORTED) in that form.  For a block whose largest finite size is s the power is the least

@@ -644,7 +644,8 @@ __global__ __launch_bounds__(NT) void draw_row_kernel(DrawArgs a)
                 from = from + step * (uint32_t)first;
                 to = hit < to && hit > from ? hit : to;
             }
-            if (key_of(floor) < from) {
+            // (<=: where top_k ends at the very score that falls short, its ties go, too)
+            if (key_of(floor) <= from) {
                 floor = of_key(from);
                 ties = 0;
             }

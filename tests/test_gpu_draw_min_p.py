@@ -47,14 +47,17 @@ def test_scores_a_step_below_the_largest_do_not_reach_all_of_its_weight(c, top_k
         assert int(drawn) == int(at.sort().values[int(u * 10)]) and abs(float(probs) - 0.1) < 1e-7
 
 
-def test_what_top_k_leaves_does_not_say_which_path_a_row_takes():
+@pytest.mark.parametrize("reach", [40, 200, 900, 3000])
+def test_what_top_k_leaves_does_not_say_which_path_a_row_takes(reach):
     """the classes that min_p leaves are the same whatever top_k is over their number"""
-    z = whole_scores(1, 30000, "bf16", 11)
-    scores = z[0].float().cpu()
-    count = {s: int((scores > scores.max() - s).sum()) for s in range(1, 20)}
-    s = next(s for s in count if count[s] >= 5)
-    u = torch.tensor([0.7], device="cuda")
-    want = ref.draw(scores.tolist(), float(u[0]), 1.0, 0, 1.0, beside(2.0 ** -s, 1))
-    for top_k in (count[s] + 1, count[s] + 100, 300, 1000, 1024, 2000, 10000, 29999):
-        drawn, probs = api.wpsgd_draw_classes(z, u, temperature=T_ONE, top_k=top_k, min_p=beside(2.0 ** -s, 1))
+    c = 30000
+    at = torch.randperm(c, generator=torch.Generator().manual_seed(reach))
+    z = torch.full((1, c), -6.0)
+    z[0, at[:reach]] = 0.0
+    z[0, at[reach:2 * reach]] = -1.0
+    u = torch.tensor([0.7])
+    want = ref.draw(z[0].tolist(), float(u[0]), 1.0, 0, 1.0, beside(0.5, 1))
+    assert want[2] == reach << 31
+    for top_k in [k for k in (50, 128, 129, 250, 300, 1000, 1024, 1025, 2000, 10000, 29999) if k >= reach]:
+        drawn, probs = api.wpsgd_draw_classes(z.bfloat16().cuda(), u.cuda(), temperature=T_ONE, top_k=top_k, min_p=beside(0.5, 1))
         assert int(drawn) == want[0] and float(probs) == float(np.float32(want[1] / want[2]))

@@ -315,7 +315,7 @@ typedef struct wpsgd_blocks {
  *              NULL: rows 0 .. n-1
  *   transpose  0: out is n x d, blocks along d.  Not 0: out is d x n, blocks along the n rows.
  *   out        its rows and cols say so; codes and exps are written, the padding of codes with 0 (not the padding of exps)
- * Errors: INVALID_ARG, UNSUPPORTED (CSR; more than 2^31 - 1 workgroups), HIP_ERROR.                                    */
+ * Errors: INVALID_ARG, UNSUPPORTED (CSR), HIP_ERROR.                                                                   */
 int wpsgd_quantize(const wpsgd_matrix *X, const int64_t *rows, int64_t n, int transpose, const wpsgd_blocks *out, void *stream);
 
 /* out[i*ld_out + j] = sum_c A(i, c) * B(j, c), for all rows i of A and j of B: summed in fp32, rounded once to dtype.  Large products
@@ -327,7 +327,8 @@ int wpsgd_quantize(const wpsgd_matrix *X, const int64_t *rows, int64_t n, int tr
  *   out        DEVICE, A->rows x B->rows; it may not overlap A or B
  *   workspace  DEVICE scratch of at least wpsgd_block_matmul_workspace(A->rows, B->rows, A->cols) bytes, 256-byte aligned
  *              (may be NULL where that is 0)
- * The result does not depend on timing.  Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, UNSUPPORTED, HIP_ERROR.              */
+ * The result does not depend on timing.  Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, UNSUPPORTED (2^31 rows or more; row strides over
+ * 4 MiB with more than 4 million rows on both sides), HIP_ERROR.                                                       */
 size_t wpsgd_block_matmul_workspace(int64_t rows_a, int64_t rows_b, int64_t cols);
 int wpsgd_block_matmul(const wpsgd_blocks *A, const wpsgd_blocks *B, void *out, int64_t ld_out, wpsgd_dtype dtype,
                        void *workspace, size_t workspace_bytes, void *stream);

@@ -640,7 +640,7 @@ static hipError_t launch_rows_of(const MatmulArgs &g, bool turned, hipStream_t s
     int along = 1;
     while (along < kRowWaves && along < kHeldBlocks / MT && groups * panels * along < 2048 && g.blocks >= 2 * along) along *= 2;
     const int64_t grid = (groups * along + kRowWaves - 1) / kRowWaves;
-    if (grid > 0x7FFFFFFFLL || panels > 65535) return hipErrorInvalidConfiguration;
+    if (grid > most_groups(64 * kRowWaves) || panels > 65535) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL((matmul_rows_kernel<MT, NT, TO>), dim3((unsigned)grid, (unsigned)panels), dim3(64 * kRowWaves), 0, s, g, along, turned);
     return hipGetLastError();
 }
@@ -696,7 +696,7 @@ int wpsgd_block_matmul(const wpsgd_blocks *A, const wpsgd_blocks *B, void *out, 
     } else {
         const int64_t side = p.kind == MatmulPlan::Tile128 ? 128 : 256;
         const int64_t tiles = ((g.M + side - 1) / side) * ((g.N + side - 1) / side);
-        if (tiles > 0x7FFFFFFFLL) return WPSGD_UNSUPPORTED;
+        if (tiles > most_groups(256)) return WPSGD_UNSUPPORTED;
         g.each = p.each;
         const dim3 grid((unsigned)tiles), block(256);
         if (p.kind == MatmulPlan::Fast256) {

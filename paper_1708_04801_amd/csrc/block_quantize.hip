@@ -39,6 +39,7 @@ struct QuantizeArgs {
     uint8_t *codes, *exps;
     int64_t ld_codes, ld_exps;
     int64_t blocks;
+    int64_t first;             // workgroup of the call at which the launch begins
 };
 
 template <typename T>
@@ -60,7 +61,7 @@ __device__ inline void load8(const T *p, int64_t left, float (&x)[8])
 template <typename T>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantizeArgs a)
 {
-    const int64_t first = (int64_t)blockIdx.x * 16;
+    const int64_t first = (a.first + blockIdx.x) * 16;
     const int64_t row0 = first / a.blocks;
     const int64_t at = (first - row0 * a.blocks) + (threadIdx.x >> 4);     // (blocks < 2^25: the sum fits 32 bits)
     const uint32_t down = (uint32_t)at / (uint32_t)a.blocks;
@@ -107,7 +108,7 @@ __global__ __launch_bounds__(256) void quantize_columns_kernel(QuantizeArgs a)
     __shared__ __attribute__((aligned(16))) T tile[kBlockCols][kCols];          // later the codes, 128 bytes to a column
     __shared__ float2 size[8][kCols / 2];
     const int64_t tiles = (a.d + kCols - 1) / kCols;
-    const int64_t b = (int64_t)blockIdx.x / tiles, col0 = ((int64_t)blockIdx.x - b * tiles) * kCols;
+    const int64_t group = a.first + blockIdx.x, b = group / tiles, col0 = (group - b * tiles) * kCols;
     const int t = threadIdx.x;
 #pragma unroll
     for (int i = 0; i < kBlockCols * kVectors / 256; ++i) {
@@ -202,20 +203,16 @@ extern "C" int wpsgd_quantize(const wpsgd_matrix *X, const int64_t *rows, int64_
     if (rc != WPSGD_OK) return rc;
     if (out->rows != (transpose ? X->d : n) || out->cols != (transpose ? n : X->d)) return WPSGD_INVALID_ARG;
     if (n == 0) return WPSGD_OK;
-    const QuantizeArgs a{X->dense, rows, X->m, X->d, X->ld, n, static_cast<uint8_t *>(out->codes), static_cast<uint8_t *>(out->exps), out->ld, out->ld_exps,
-                         (out->cols + kBlockCols - 1) / kBlockCols};
+    QuantizeArgs a{X->dense, rows, X->m, X->d, X->ld, n, static_cast<uint8_t *>(out->codes), static_cast<uint8_t *>(out->exps), out->ld, out->ld_exps,
+                         (out->cols + kBlockCols - 1) / kBlockCols, 0};
     const int64_t groups = transpose ? a.blocks * ((X->d + 63) / 64) : (n * a.blocks + 15) / 16;
-    if (groups > 0x7FFFFFFFLL) return WPSGD_UNSUPPORTED;
-    const dim3 grid((unsigned)groups), block(256);
     hipStream_t s = static_cast<hipStream_t>(stream);
     const bool half = X->dtype == WPSGD_BF16;
-    if (transpose) {
-        if (half) hipLaunchKernelGGL(quantize_columns_kernel<uint16_t>, grid, block, 0, s, a);
-        else hipLaunchKernelGGL(quantize_columns_kernel<float>, grid, block, 0, s, a);
-    } else {
-        if (half) hipLaunchKernelGGL(quantize_rows_kernel<uint16_t>, grid, block, 0, s, a);
-        else hipLaunchKernelGGL(quantize_rows_kernel<float>, grid, block, 0, s, a);
-    }
-    const hipError_t e = hipGetLastError();
+    const auto kernel = transpose ? (half ? quantize_columns_kernel<uint16_t> : quantize_columns_kernel<float>)
+                                  : (half ? quantize_rows_kernel<uint16_t> : quantize_rows_kernel<float>);
+    const hipError_t e = in_launches(groups, 256, [&](int64_t first, unsigned count) {
+        a.first = first;
+        hipLaunchKernelGGL(kernel, dim3(count), dim3(256), 0, s, a);
+    });
     return e == hipSuccess ? WPSGD_OK : hip_fail(e);
 }

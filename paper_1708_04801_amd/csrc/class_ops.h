@@ -56,4 +56,19 @@ __device__ inline float wave_max(float v)
     return fmaxf(v, __shfl_xor(v, 32));
 }
 
+// A launch has fewer than 2^32 threads along x.
+constexpr int64_t most_groups(int threads) { return 0xFFFFFFFFLL / threads; }
+// Any number of workgroups, in as many launches as that takes: run(first, count) queues one.
+template <typename F>
+inline hipError_t in_launches(int64_t groups, int threads, F &&run)
+{
+    const int64_t most = most_groups(threads);
+    for (int64_t first = 0; first < groups; first += most) {
+        run(first, (unsigned)(groups - first < most ? groups - first : most));
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
 }  // namespace wpsgd

@@ -19,6 +19,7 @@ struct DrawArgs {
     wpsgd_draw_rule rule;
     int64_t *classes;
     float *probs;
+    int64_t first;             // row at which the launch begins
 };
 
 constexpr float kOne = 2147483648.0f;           // the largest score's weight
@@ -406,7 +407,7 @@ __global__ __launch_bounds__(NT) void draw_row_kernel(DrawArgs a)
     constexpr float kInf = __builtin_inff();
     __shared__ typename R::Shared sh;
     R row;
-    const int64_t at_row = blockIdx.x;
+    const int64_t at_row = a.first + blockIdx.x;
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     row.sh = &sh;
     row.z = static_cast<const T *>(a.z) + at_row * a.ld;
@@ -907,14 +908,16 @@ __global__ __launch_bounds__(NT) void draw_row_kernel(DrawArgs a)
 }
 
 template <typename T>
-static hipError_t launch_draw(const DrawArgs &a, hipStream_t s)
+static hipError_t launch_draw(DrawArgs a, hipStream_t s)
 {
-    const dim3 grid((unsigned)a.n);
     // short rows: four waves, whose barriers are shorter, and several workgroups to a compute unit (us a call with top_p 0.9, four waves | sixteen, bfloat16: 200 rows of
     // 8000 16.4 | 20.8, one of 16000 17.5 | 21.4, but fp32, 200 of 16000 28.8 | 22.8, and with top 50 13.4 | 11.2)
-    if (a.c <= 8192) hipLaunchKernelGGL((draw_row_kernel<T, 256, 2048>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((draw_row_kernel<T, 1024, 14336>), grid, dim3(1024), 0, s, a);
-    return hipGetLastError();
+    const bool few = a.c <= 8192;
+    return in_launches(a.n, few ? 256 : 1024, [&](int64_t first, unsigned count) {
+        a.first = first;
+        if (few) hipLaunchKernelGGL((draw_row_kernel<T, 256, 2048>), dim3(count), dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((draw_row_kernel<T, 1024, 14336>), dim3(count), dim3(1024), 0, s, a);
+    });
 }
 
 }  // namespace wpsgd
@@ -933,7 +936,7 @@ int wpsgd_draw_classes(const void *Z, int64_t n, int64_t classes, int64_t ld, wp
     if (n == 0) return WPSGD_OK;
     const size_t elem = dtype == WPSGD_F32 ? 4 : 2;
     if (!Z || !u || !drawn || ld < classes || (uintptr_t)Z % elem != 0) return WPSGD_INVALID_ARG;
-    const DrawArgs a{Z, n, classes, ld, u, *rule, drawn, probs};
+    const DrawArgs a{Z, n, classes, ld, u, *rule, drawn, probs, 0};
     hipStream_t s = static_cast<hipStream_t>(stream);
     const hipError_t e = dtype == WPSGD_F32 ? launch_draw<float>(a, s) : launch_draw<uint16_t>(a, s);
     return e == hipSuccess ? WPSGD_OK : hip_fail(e);

@@ -14,6 +14,7 @@ struct LossArgs {
     float *loss;
     void *grad;
     int64_t ld_grad;
+    int64_t first;             // workgroup of the call at which the launch begins
 };
 
 constexpr float kLog2e = 1.44269504088896340736f;
@@ -28,7 +29,7 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void softmax_row_kernel(LossAr
     constexpr int E = Elem<T>::kPer16, kRows = NT < 256 ? 256 / NT : 1, kWaves = NT / 64;
     constexpr float kInf = __builtin_inff();
     __shared__ float part[2][kWaves];
-    const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / NT;
+    const int64_t row = (a.first + blockIdx.x) * kRows + threadIdx.x / NT;
     if (kRows > 1 && row >= a.n) return;                                          // (whole waves)
     const int t = threadIdx.x % NT;
     const T *z = static_cast<const T *>(a.z) + row * a.ld;
@@ -141,12 +142,14 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void softmax_row_kernel(LossAr
 }
 
 template <typename T>
-static hipError_t launch_loss(const LossArgs &a, hipStream_t s)
+static hipError_t launch_loss(LossArgs a, hipStream_t s)
 {
     const int64_t vectors = a.c / Elem<T>::kPer16;
     const auto run = [&](auto kernel, int64_t groups, int threads) {
-        hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(threads), 0, s, a);
-        return hipGetLastError();
+        return in_launches(groups, threads, [&](int64_t first, unsigned count) {
+            a.first = first;
+            hipLaunchKernelGGL(kernel, dim3(count), dim3(threads), 0, s, a);
+        });
     };
     // the fewest threads whose registers hold a row; rows that half the registers of a compute unit cannot hold are its only one
     if (vectors <= 64 * 4) return run(softmax_row_kernel<T, 64, 4, false>, (a.n + 3) / 4, 256);
@@ -174,7 +177,7 @@ int wpsgd_softmax_loss(const void *Z, int64_t n, int64_t classes, int64_t ld, wp
     if (grad && (ld_grad < classes || (uintptr_t)grad % elem != 0)) return WPSGD_INVALID_ARG;
     if (grad == Z && ld_grad != ld) return WPSGD_INVALID_ARG;
     if (!(scale - scale == 0.0)) return WPSGD_INVALID_ARG;
-    const LossArgs a{Z, n, classes, ld, labels, row_weights, (float)scale, loss, grad, ld_grad};
+    const LossArgs a{Z, n, classes, ld, labels, row_weights, (float)scale, loss, grad, ld_grad, 0};
     hipStream_t s = static_cast<hipStream_t>(stream);
     const hipError_t e = dtype == WPSGD_F32 ? launch_loss<float>(a, s) : launch_loss<uint16_t>(a, s);
     return e == hipSuccess ? WPSGD_OK : hip_fail(e);

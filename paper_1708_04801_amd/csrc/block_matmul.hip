@@ -6,6 +6,7 @@
 // powers of ten) of the result's norm, where fp32 sums are off by 1e-7.
 #include <type_traits>
 
+#include "block_plan.h"
 #include "class_ops.h"
 
 namespace wpsgd {
@@ -605,31 +606,6 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const float *parts, int
     }
 }
 
-// Which kernel, by sizes and the results' type alone.  Few rows: the one that reads the others once.  Else the one that should take the least time (us, measured for 1024 x 1024
-// to 16384 x 4096 results and 4 to 64 blocks of the sum): a round of tiles on all compute units takes 0.98 a block for 128 x 128 (two workgroups to a unit, so that
-// one's products hide the other's loads and results), 2.2 for 256 x 256 with fp32 sums and 1.09 in the 8-bit instruction (one to a unit, results not
-// hidden).  4096 x 4096, 8 blocks: fp32 41 | 38 (128 | 256), bfloat16 43 | 26; 5003 x 3001, 8 blocks, fp32: 38 | 42; 2048 x 2048, 64 blocks: 64 | 80 (8-bit).
-struct MatmulPlan {
-    enum { Rows, Tile128, Tile256, Fast256 } kind;
-    int parts, each;           // Tile128: parts of the sum and blocks to each
-};
-static MatmulPlan plan_matmul(int64_t M, int64_t N, int64_t blocks, bool f32, bool wide_rows)
-{
-    const int64_t few = M < N ? M : N;
-    if (few <= 64 || wide_rows) return {MatmulPlan::Rows, 1, 0};
-    if (blocks == 0) return {MatmulPlan::Tile128, 0, 0};                      // a sum over nothing
-    const int64_t t256 = ((M + 255) / 256) * ((N + 255) / 256), t128 = ((M + 127) / 128) * ((N + 127) / 128);
-    int parts = 1;
-    while (t128 * parts < 256 && blocks >= parts * 16) parts *= 2;           // eight blocks to a part at least
-    const int each = parts == 1 ? (int)blocks : (int)(((blocks + parts - 1) / parts + 3) / 4 * 4);
-    parts = (int)((blocks + each - 1) / each);
-    const double out = (double)M * (double)N * (f32 ? 4.0 : 2.0) / 4.6e6;    // to write the results
-    const auto rounds = [](int64_t tiles) { return tiles < 256 ? 1.0 : (double)tiles / 256.0; };
-    const double by128 = 5.0 + 0.98 * each * rounds(t128 * parts) + 0.5 * out + (parts > 1 ? 4.0 : 0.0);
-    const double by256 = (f32 ? 13.0 + 2.2 * (double)blocks * rounds(t256) : 10.0 + 1.09 * (double)blocks * rounds(t256)) + out;
-    if (by256 < by128) return {f32 ? MatmulPlan::Tile256 : MatmulPlan::Fast256, 1, (int)blocks};
-    return {MatmulPlan::Tile128, parts, each};
-}
 static size_t parts_bytes(const MatmulPlan &p, int64_t M, int64_t N) { return p.parts > 1 ? ((size_t)p.parts * M * N * sizeof(float) + 255) & ~(size_t)255 : 0; }
 
 template <int MT, int NT, typename TO>
@@ -647,15 +623,11 @@ static hipError_t launch_rows_of(const MatmulArgs &g, bool turned, hipStream_t s
 template <typename TO>
 static hipError_t launch_rows(const MatmulArgs &g, hipStream_t s)
 {
-    const bool turned = g.M > g.N;
-    const int64_t many = turned ? g.M : g.N, few = turned ? g.N : g.M;
-    // too few rows for the compute units: the few rows in sixteens beside each other, too (64 x 1000 x 4096: 28 us without that)
-    if (few <= 16 || many <= 2048) return many >= 32 * 2048 ? launch_rows_of<1, 2, TO>(g, turned, s) : launch_rows_of<1, 1, TO>(g, turned, s);
-    if (few <= 32) return many >= 32 * 2048 ? launch_rows_of<2, 2, TO>(g, turned, s) : launch_rows_of<2, 1, TO>(g, turned, s);
-    return many >= 32 * 2048 ? launch_rows_of<4, 2, TO>(g, turned, s) : launch_rows_of<4, 1, TO>(g, turned, s);
+    const RowsShape r = rows_shape(g.M, g.N);
+    if (r.mt == 1) return r.nt == 2 ? launch_rows_of<1, 2, TO>(g, r.turned, s) : launch_rows_of<1, 1, TO>(g, r.turned, s);
+    if (r.mt == 2) return r.nt == 2 ? launch_rows_of<2, 2, TO>(g, r.turned, s) : launch_rows_of<2, 1, TO>(g, r.turned, s);
+    return r.nt == 2 ? launch_rows_of<4, 2, TO>(g, r.turned, s) : launch_rows_of<4, 1, TO>(g, r.turned, s);
 }
-// rows of a tile are addressed with 32 bits
-static bool wide(int64_t ld, int64_t ld_exps) { return ld > (1LL << 22) || ld_exps > (1LL << 22); }
 
 }  // namespace wpsgd
 

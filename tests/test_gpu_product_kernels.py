@@ -22,7 +22,7 @@ def blocks(t, **how):
 def values(q):
     """what the blocks stand for, in 64 bits"""
     b = q.codes.shape[1] // 128
-    power = torch.ldexp(torch.ones((), dtype=torch.float64, device="cuda"), q.exps[:, :b].to(torch.int32) - 127)
+    power = ((q.exps[:, :b].to(torch.int64) + (1023 - 127)) << 52).view(torch.float64)
     return (q.codes.to(torch.float64).view(q.rows, b, 128) * power[..., None]).view(q.rows, b * 128)
 
 

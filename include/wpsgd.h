@@ -303,7 +303,7 @@ typedef struct wpsgd_blocks {
     int64_t rows, cols;        /* 0 <= cols <= 2^31                                                       */
     void *codes;               /* DEVICE, one byte each, 16-byte aligned                                  */
     int64_t ld;                /* row stride in bytes, a multiple of 16, >= 128*ceil(cols/128)            */
-    void *exps;                /* DEVICE, one byte (1 .. 254) for each block, 4-byte aligned              */
+    void *exps;                /* DEVICE, one byte (1 .. 247: all that fp32 values need) for each block, 4-byte aligned */
     int64_t ld_exps;           /* row stride in bytes, a multiple of 4, >= ceil(cols/128); products read whole
                                   words of each row, the last one's too                                   */
 } wpsgd_blocks;
@@ -320,7 +320,8 @@ int wpsgd_quantize(const wpsgd_matrix *X, const int64_t *rows, int64_t n, int tr
 
 /* out[i*ld_out + j] = sum_c A(i, c) * B(j, c), for all rows i of A and j of B: summed in fp32, rounded once to dtype.  Large products
  * to bfloat16 go through the 8-bit matrix instructions, which of a few products at a time keep what lies within 2^14 of the
- * largest: 1e-5 to 7e-5 of a result's usual size, where the type's own rounding is 2e-3.  Results are NaN where a row has a NaN.
+ * largest: 1e-5 to 7e-5 of a result's usual size, where the type's own rounding is 2e-3.  Results are NaN where a row has a NaN
+ * (or sums that fp32 cannot hold cancel).  Elements under 2^-126 may be rounded to multiples of 2^-132.
  * With x the rows of a batch (n x d), W the class vectors (classes x d) and G the loss gradient (n x classes):
  *   scores              A = x, B = W                 gradient of W      A = G transposed, B = x transposed
  *   gradient of x       A = G, B = W transposed      (transposed: as wpsgd_quantize makes it)

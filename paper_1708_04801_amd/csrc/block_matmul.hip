@@ -1,9 +1,10 @@
 // Scores: out[i,j] = sum over blocks b of 2^(ea[i,b] + eb[j,b]) * sum_k A[i,b,k] B[j,b,k], rounded once to the output's type.
 //
-// Sums of fp32 accuracy: codes become bfloat16 in registers, their block's power of two in the same instruction (four significant bits
-// and the exponent both fit), and go to the bfloat16 matrix instruction, which adds in fp32.  The 8-bit matrix instructions are twice as fast, but
-// inside a group of products they keep only what lies within 2^14 of the largest: 1.5e-5 (normal values) to 7e-5 (values over several
-// powers of ten) of the result's norm, where fp32 sums are off by 1e-7.
+// Sums of fp32 accuracy: codes become bfloat16 in registers, their block's power of two in the same instruction, and go to the bfloat16 matrix instruction, which
+// adds in fp32.  Four significant bits fit, and the exponents of all fp32 values do with half the power: 1.94 * 2^127 and more has code 256 at 2^120, and 2^128
+// would be infinite.  Results are taken times four at the end.  Exact for exponent bytes 4 to 247; with 1 to 3, bfloat16's subnormal spacing rounds values to multiples of 2^-132.
+// The 8-bit matrix instructions are twice as fast, but inside a group of products they keep only what lies within 2^14 of the largest: 1.5e-5 (normal
+// values) to 7e-5 (values over several powers of ten) of the result's norm, where fp32 sums are off by 1e-7.
 #include <type_traits>
 
 #include "block_plan.h"
@@ -27,7 +28,9 @@ struct MatmulArgs {
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-__device__ inline float power_of(int byte) { return __uint_as_float((uint32_t)byte << 23); }
+// half a block's power of two (the instruction takes the exponent field 0, for byte 1, as 2^-127)
+__device__ inline float half_power_of(int byte) { return __uint_as_float(((uint32_t)byte << 23) - (1u << 23)); }
+constexpr float kHalves = 4.0f;        // what products of two halves are short of
 
 // eight codes, two words, times a power of two
 __device__ inline bf16x8 widen8(uint32_t lo, uint32_t hi, float scale)
@@ -123,8 +126,8 @@ __global__ __launch_bounds__(64 * kRowWaves) void matmul_rows_kernel(MatmulArgs 
 #pragma unroll
                 for (int x = 0; x < kItems; ++x) {
                     const int item = wave + x * kRowWaves;
-                    lds.held[(item >> 1) * 4 + (item & 1) * 2][lane] = widen8(q[x].x, q[x].y, power_of(c[x]));
-                    lds.held[(item >> 1) * 4 + (item & 1) * 2 + 1][lane] = widen8(q[x].z, q[x].w, power_of(c[x]));
+                    lds.held[(item >> 1) * 4 + (item & 1) * 2][lane] = widen8(q[x].x, q[x].y, half_power_of(c[x]));
+                    lds.held[(item >> 1) * 4 + (item & 1) * 2 + 1][lane] = widen8(q[x].z, q[x].w, half_power_of(c[x]));
                 }
                 __syncthreads();
             }
@@ -133,7 +136,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void matmul_rows_kernel(MatmulArgs 
                 bf16x8 fs[NT][4];
 #pragma unroll
                 for (int u = 0; u < NT; ++u) {
-                    const float c = power_of(cs[j][u]);
+                    const float c = half_power_of(cs[j][u]);
                     fs[u][0] = widen8(qs[j][u][0].x, qs[j][u][0].y, c);
                     fs[u][1] = widen8(qs[j][u][0].z, qs[j][u][0].w, c);
                     fs[u][2] = widen8(qs[j][u][1].x, qs[j][u][1].y, c);
@@ -167,6 +170,10 @@ __global__ __launch_bounds__(64 * kRowWaves) void matmul_rows_kernel(MatmulArgs 
                 for (int w = 1; w < along; ++w) acc[t][u] += lds.sums[wave + w][t * NT + u][lane];
     }
     if (idle) return;
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int u = 0; u < NT; ++u) acc[t][u] *= kHalves;
     TO *out = static_cast<TO *>(g.out);
 #pragma unroll
     for (int t = 0; t < MT; ++t)
@@ -280,7 +287,7 @@ struct Tile {
     // A wave's results, 32 rows at a time, through LDS of its own (32 rows of 32 TN results), so that whole rows of 128 bytes and more go out: with what
     // a lane holds (four results side by side) 32 bytes of a row at a time, bfloat16 results cost 0.8 ms per GiB on top of the products.
     template <typename TO>
-    __device__ void store(const MatmulArgs &g, f32x16 (&acc)[TM][TN], uint8_t *room) const
+    __device__ void store(const MatmulArgs &g, f32x16 (&acc)[TM][TN], float times, uint8_t *room) const
     {
         constexpr int kRow = 32 * TN * (int)sizeof(TO), kPieces = kRow / 16, E = Elem<TO>::kPer16;
         static_assert(kPieces >= 8, "pieces of a row are permuted within eight");
@@ -293,7 +300,7 @@ struct Tile {
             for (int u = 0; u < TN; ++u)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const float x0 = acc[t][u][q * 4], x1 = acc[t][u][q * 4 + 1], x2 = acc[t][u][q * 4 + 2], x3 = acc[t][u][q * 4 + 3];
+                    const float x0 = acc[t][u][q * 4] * times, x1 = acc[t][u][q * 4 + 1] * times, x2 = acc[t][u][q * 4 + 2] * times, x3 = acc[t][u][q * 4 + 3] * times;
                     if constexpr (E == 8) {
                         const int piece = u * 4 + q;
                         *reinterpret_cast<uint2 *>(room + m * kRow + ((piece ^ (m & 7)) * 16) + half * 8) = make_uint2(bf16_pack(x0, x1), bf16_pack(x2, x3));
@@ -371,7 +378,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM * TN > 8
         return *reinterpret_cast<const uint4 *>(lds + (b & 1) * kStage + row * 128 + (((part * 2 + half) ^ ((r >> 1) & 7)) * 16));
     };
     auto scale = [&](int row, int b) -> float {
-        return power_of(lds[2 * kStage + ((b >> 2) & 1) * G::kExps + row * 4 + (b & 3)]);
+        return half_power_of(lds[2 * kStage + ((b >> 2) & 1) * G::kExps + row * 4 + (b & 3)]);
     };
     bf16x8 fa[2][2], fb[TN][2];
     uint4 qa[2], qb[TN];
@@ -447,7 +454,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(TM * TN > 8
             }
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
-    tile.template store<TO>(g, acc, lds + wave * (32 * 32 * TN * (int)sizeof(TO)));
+    tile.template store<TO>(g, acc, kHalves, lds + wave * (32 * 32 * TN * (int)sizeof(TO)));
 }
 
 // Products in the 8-bit matrix instruction, which takes the exponent bytes with it: twice the rate, sums as said at the top, so for bfloat16 results only.
@@ -573,7 +580,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
         slot = slot2;
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
-    tile.template store<uint16_t>(g, acc, lds + wave * (32 * 32 * TN * 2));
+    tile.template store<uint16_t>(g, acc, 1.0f, lds + wave * (32 * 32 * TN * 2));
 }
 
 // The parts of a split sum, added in their order and rounded once.

@@ -320,7 +320,8 @@ int wpsgd_quantize(const wpsgd_matrix *X, const int64_t *rows, int64_t n, int tr
 
 /* out[i*ld_out + j] = sum_c A(i, c) * B(j, c), for all rows i of A and j of B: summed in fp32, rounded once to dtype.  Large products
  * to bfloat16 go through the 8-bit matrix instructions, which of a few products at a time keep what lies within 2^14 of the
- * largest: 1e-5 to 7e-5 of a result's usual size, where the type's own rounding is 2e-3.  Results are NaN where a row has a NaN
+ * largest: 1e-5 to 7e-5 of a result's usual size, where the type's own rounding is 2e-3.  Where large products cancel and small ones
+ * are what counts, ask for WPSGD_BF16 | WPSGD_FP32_SUMS: bfloat16 results of sums in fp32 at any size.  Results are NaN where a row has a NaN
  * (or sums that fp32 cannot hold cancel).  Elements under 2^-126 may be rounded to multiples of 2^-132.
  * With x the rows of a batch (n x d), W the class vectors (classes x d) and G the loss gradient (n x classes):
  *   scores              A = x, B = W                 gradient of W      A = G transposed, B = x transposed
@@ -331,7 +332,8 @@ int wpsgd_quantize(const wpsgd_matrix *X, const int64_t *rows, int64_t n, int tr
  * The result does not depend on timing.  Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, UNSUPPORTED (2^31 rows or more; row strides over
  * 4 MiB with more than 4 million rows on both sides), HIP_ERROR.                                                       */
 size_t wpsgd_block_matmul_workspace(int64_t rows_a, int64_t rows_b, int64_t cols);
-int wpsgd_block_matmul(const wpsgd_blocks *A, const wpsgd_blocks *B, void *out, int64_t ld_out, wpsgd_dtype dtype,
+#define WPSGD_FP32_SUMS 16     /* with the dtype of wpsgd_block_matmul's results */
+int wpsgd_block_matmul(const wpsgd_blocks *A, const wpsgd_blocks *B, void *out, int64_t ld_out, int dtype_and_sums,
                        void *workspace, size_t workspace_bytes, void *stream);
 
 /* Softmax cross-entropy of n rows of scores, and its gradient:

@@ -20,6 +20,7 @@ LIB_PATH = os.path.join(_PKG, "libwpsgd.so")
 HINGE, LOGISTIC = 0, 1
 SAMPLE_STREAM, SAMPLE_SHARDS = 0, 1
 F32, BF16 = 0, 1
+FP32_SUMS = 16
 OK, INVALID_ARG, HIP_ERROR, WORKSPACE_TOO_SMALL, UNSUPPORTED, INCOMPLETE = 0, -1, -2, -3, -4, -5
 
 EXPORTS = [
@@ -596,15 +597,16 @@ def wpsgd_block_matmul_workspace(rows_a, rows_b, cols) -> int:
 
 
 def wpsgd_block_matmul(A: BlockMatrix, B: BlockMatrix, out: Optional[torch.Tensor] = None, dtype=torch.bfloat16,
-                       workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-    """out[i, j] = sum_c A[i, c] B[j, c], float32 or bfloat16."""
+                       workspace: Optional[torch.Tensor] = None, stream=None, fp32_sums=False) -> torch.Tensor:
+    """out[i, j] = sum_c A[i, c] B[j, c], float32 or bfloat16.  fp32_sums: bfloat16 results of fp32 sums at large sizes, too, where the 8-bit
+    matrix instructions would otherwise drop products under 2^-14 of the largest of their 64."""
     if out is None:
         out = _new(A.codes, (A.rows, B.rows), dtype, stream)
     assert out.is_cuda and out.dtype in _DTYPES and out.shape == (A.rows, B.rows) and (out.numel() == 0 or out.stride(1) == 1)
     L = load()
     p, size, held = _call_workspace(workspace, L.wpsgd_block_matmul_workspace(A.rows, B.rows, A.cols), out, stream)
     rc = L.wpsgd_block_matmul(ctypes.byref(A.c_struct()), ctypes.byref(B.c_struct()), out.data_ptr(), out.stride(0) if A.rows > 1 else max(out.stride(0), B.rows),
-                              _DTYPES[out.dtype], p, size, _stream_of(stream, out))
+                              _DTYPES[out.dtype] | (FP32_SUMS if fp32_sums else 0), p, size, _stream_of(stream, out))
     if rc != OK:
         raise WpsgdError(rc, "wpsgd_block_matmul")
     return out

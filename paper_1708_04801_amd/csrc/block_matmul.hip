@@ -4,7 +4,8 @@
 // adds in fp32.  Four significant bits fit, and the exponents of all fp32 values do with half the power: 1.94 * 2^127 and more has code 256 at 2^120, and 2^128
 // would be infinite.  Results are taken times four at the end.  Exact for exponent bytes 4 to 247; with 1 to 3, bfloat16's subnormal spacing rounds values to multiples of 2^-132.
 // The 8-bit matrix instructions are twice as fast, but inside a group of products they keep only what lies within 2^14 of the largest: 1.5e-5 (normal
-// values) to 7e-5 (values over several powers of ten) of the result's norm, where fp32 sums are off by 1e-7.
+// values) to 7e-5 (values over several powers of ten) of the result's norm, where fp32 sums are off by 1e-7.  So they are for bfloat16 results only, and a call may ask for
+// fp32 sums of those, too (8192 x 65536 x 4096 3070 us instead of 1860).
 #include <type_traits>
 
 #include "block_plan.h"
@@ -645,18 +646,25 @@ extern "C" {
 size_t wpsgd_block_matmul_workspace(int64_t rows_a, int64_t rows_b, int64_t cols)
 {
     if (rows_a <= 0 || rows_b <= 0 || cols <= 0) return 0;
-    // (whatever the results' type)
+    // (whatever the results' type and sums)
     const int64_t blocks = (cols + 127) / 128;
-    const size_t a = parts_bytes(plan_matmul(rows_a, rows_b, blocks, true, false), rows_a, rows_b), b = parts_bytes(plan_matmul(rows_a, rows_b, blocks, false, false), rows_a, rows_b);
-    return a > b ? a : b;
+    size_t most = 0;
+    for (int f32 = 0; f32 < 2; ++f32)
+        for (int sums = 0; sums < 2; ++sums) {
+            const size_t one = parts_bytes(plan_matmul(rows_a, rows_b, blocks, f32 != 0, false, sums != 0), rows_a, rows_b);
+            most = one > most ? one : most;
+        }
+    return most;
 }
 
-int wpsgd_block_matmul(const wpsgd_blocks *A, const wpsgd_blocks *B, void *out, int64_t ld_out, wpsgd_dtype dtype, void *workspace, size_t workspace_bytes,
+int wpsgd_block_matmul(const wpsgd_blocks *A, const wpsgd_blocks *B, void *out, int64_t ld_out, int dtype_and_sums, void *workspace, size_t workspace_bytes,
                        void *stream)
 {
     int rc = check_blocks(A);
     if (rc == WPSGD_OK) rc = check_blocks(B);
     if (rc != WPSGD_OK) return rc;
+    const int dtype = dtype_and_sums & ~WPSGD_FP32_SUMS;
+    const bool sums = (dtype_and_sums & WPSGD_FP32_SUMS) != 0;
     if (A->cols != B->cols || (dtype != WPSGD_F32 && dtype != WPSGD_BF16)) return WPSGD_INVALID_ARG;
     if (A->rows == 0 || B->rows == 0) return WPSGD_OK;
     if (!out || ld_out < B->rows || (uintptr_t)out % (dtype == WPSGD_F32 ? 4 : 2) != 0) return WPSGD_INVALID_ARG;
@@ -666,7 +674,7 @@ int wpsgd_block_matmul(const wpsgd_blocks *A, const wpsgd_blocks *B, void *out, 
     MatmulArgs g{static_cast<const uint8_t *>(A->codes), static_cast<const uint8_t *>(B->codes), static_cast<const uint8_t *>(A->exps),
                  static_cast<const uint8_t *>(B->exps), A->ld, B->ld, A->ld_exps, B->ld_exps, A->rows, B->rows, (int)((A->cols + 127) / 128), out, ld_out, 0};
     const bool f32 = dtype == WPSGD_F32;
-    const MatmulPlan p = plan_matmul(g.M, g.N, g.blocks, f32, wide(g.lda, g.lde_a) || wide(g.ldb, g.lde_b));
+    const MatmulPlan p = plan_matmul(g.M, g.N, g.blocks, f32, wide(g.lda, g.lde_a) || wide(g.ldb, g.lde_b), sums);
     hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t e = hipSuccess;
     if (p.kind == MatmulPlan::Rows) {
@@ -681,7 +689,8 @@ int wpsgd_block_matmul(const wpsgd_blocks *A, const wpsgd_blocks *B, void *out, 
         if (p.kind == MatmulPlan::Fast256) {
             hipLaunchKernelGGL(matmul_fast_kernel, grid, block, 0, s, g);
         } else if (p.kind == MatmulPlan::Tile256) {
-            hipLaunchKernelGGL((matmul_tile_kernel<4, 4, float>), grid, block, 0, s, g);
+            if (f32) hipLaunchKernelGGL((matmul_tile_kernel<4, 4, float>), grid, block, 0, s, g);
+            else hipLaunchKernelGGL((matmul_tile_kernel<4, 4, uint16_t>), grid, block, 0, s, g);
         } else if (p.parts == 1) {
             if (f32) hipLaunchKernelGGL((matmul_tile_kernel<2, 2, float>), grid, block, 0, s, g);
             else hipLaunchKernelGGL((matmul_tile_kernel<2, 2, uint16_t>), grid, block, 0, s, g);

@@ -13,8 +13,10 @@ struct MatmulPlan {
     enum { Rows, Tile128, Tile256, Fast256 } kind;
     int parts, each;           // Tile128: parts of the sum and blocks to each
 };
-inline MatmulPlan plan_matmul(int64_t M, int64_t N, int64_t blocks, bool f32, bool wide_rows)
+// f32: results in fp32, whose sums are, too; f32_sums: the sums of bfloat16 results as well
+inline MatmulPlan plan_matmul(int64_t M, int64_t N, int64_t blocks, bool f32, bool wide_rows, bool f32_sums = false)
 {
+    f32_sums = f32_sums || f32;
     const int64_t few = M < N ? M : N;
     if (few <= 64 || wide_rows) return {MatmulPlan::Rows, 1, 0};
     if (blocks == 0) return {MatmulPlan::Tile128, 0, 0};                      // a sum over nothing
@@ -26,8 +28,8 @@ inline MatmulPlan plan_matmul(int64_t M, int64_t N, int64_t blocks, bool f32, bo
     const double out = (double)M * (double)N * (f32 ? 4.0 : 2.0) / 4.6e6;    // to write the results
     const auto rounds = [](int64_t tiles) { return tiles < 256 ? 1.0 : (double)tiles / 256.0; };
     const double by128 = 5.0 + 0.98 * each * rounds(t128 * parts) + 0.5 * out + (parts > 1 ? 4.0 : 0.0);
-    const double by256 = (f32 ? 13.0 + 2.2 * (double)blocks * rounds(t256) : 10.0 + 1.09 * (double)blocks * rounds(t256)) + out;
-    if (by256 < by128) return {f32 ? MatmulPlan::Tile256 : MatmulPlan::Fast256, 1, (int)blocks};
+    const double by256 = (f32_sums ? 13.0 + 2.2 * (double)blocks * rounds(t256) : 10.0 + 1.09 * (double)blocks * rounds(t256)) + out;
+    if (by256 < by128) return {f32_sums ? MatmulPlan::Tile256 : MatmulPlan::Fast256, 1, (int)blocks};
     return {MatmulPlan::Tile128, parts, each};
 }
 

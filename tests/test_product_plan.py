@@ -21,16 +21,16 @@ def plan(tmp_path_factory):
     at = tmp_path_factory.mktemp("plan")
     source, lib = str(at / "plan.cc"), str(at / "plan.so")
     with open(source, "w") as f:
-        f.write('#include "block_plan.h"\nextern "C" void plan(int64_t m, int64_t n, int64_t blocks, int f32, int wide_rows, int *o)\n{\n'
-                "    const auto p = wpsgd::plan_matmul(m, n, blocks, f32 != 0, wide_rows != 0);\n    const auto r = wpsgd::rows_shape(m, n);\n"
+        f.write('#include "block_plan.h"\nextern "C" void plan(int64_t m, int64_t n, int64_t blocks, int f32, int wide_rows, int sums, int *o)\n{\n'
+                "    const auto p = wpsgd::plan_matmul(m, n, blocks, f32 != 0, wide_rows != 0, sums != 0);\n    const auto r = wpsgd::rows_shape(m, n);\n"
                 "    const int v[] = {(int)p.kind, p.parts, p.each, r.mt, r.nt, (int)r.turned};\n    for (int i = 0; i < 6; ++i) o[i] = v[i];\n}\n")
     subprocess.run([cxx, "-std=c++17", "-O1", "-shared", "-fPIC", "-I" + build.CSRC, source, "-o", lib], check=True)
     f = ctypes.CDLL(lib).plan
-    f.argtypes = [ctypes.c_int64] * 3 + [ctypes.c_int] * 2 + [ctypes.c_void_p]
+    f.argtypes = [ctypes.c_int64] * 3 + [ctypes.c_int] * 3 + [ctypes.c_void_p]
 
-    def call(m, n, k, f32, wide=False):
+    def call(m, n, k, f32, wide=False, sums=False):
         o = (ctypes.c_int * 6)()
-        f(m, n, -(-k // 128), f32, wide, o)
+        f(m, n, -(-k // 128), f32, wide, sums, o)
         return dict(kind=KINDS[o[0]], parts=o[1], each=o[2], sixteens=(o[3], o[4]), turned=bool(o[5]))
     return call
 
@@ -72,3 +72,10 @@ def test_parts_cover_the_sum(plan):
 
 def test_wide_rows_go_where_addresses_are_64_bits(plan):
     assert plan(5000, 5000, 4096, F32, wide=True)["kind"] == plan(5000, 5000, 4096, BF16, wide=True)["kind"] == "rows"
+
+
+def test_sums_asked_for(plan):
+    for m, n, k in shapes.FAST_256:
+        assert plan(m, n, k, BF16, sums=True)["kind"] in ("tile128", "tile256")
+    for m, n, k in shapes.TILES_256:
+        assert plan(m, n, k, F32, sums=True) == plan(m, n, k, F32) and plan(m, n, k, BF16, sums=True)["kind"] == "tile256"

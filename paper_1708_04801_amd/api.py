@@ -517,12 +517,36 @@ def wpsgd_stream_rows(X: Matrix, groups, rows_per_group, seed=0, stream=None) ->
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
 
-def _stream_of(stream, t):
-    """The stream's handle; for None that of the current stream of t's device.  (These calls are short enough for the 2.6 us that
-    torch.cuda.current_stream takes to make an object of it to matter.)"""
-    if stream is None:
-        return torch._C._cuda_getCurrentRawStream(t.device.index)
+# What torch.cuda.current_stream(i).cuda_stream gives, without the 2.6 us that it takes to make an object of it; not a public name of torch, so where a torch has it no more the
+# object is made.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = torch.cuda.current_device
+
+
+def _handle(stream):
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _beside(like, *tensors):
+    """The index of like's GPU, on which all the others have to be (None: not given)."""
+    index = like.get_device()
+    for t in tensors:
+        assert t is None or t.get_device() == index, "operands on different devices"
+    return index
+
+
+def _call(f, index, stream, *args):
+    """f(*args, the stream's handle), for None that of the GPU's current stream, with that GPU as the current device: a launch goes to that, and so does the
+    stream 0."""
+    if stream is None:
+        handle = _raw_stream(index)
+    else:
+        assert getattr(stream, "device_index", index) == index, "a stream of another device"
+        handle = _handle(stream)
+    if index == _current_device():
+        return f(*args, handle)
+    with torch.cuda.device(index):
+        return f(*args, handle)
 
 
 def _new(like, shape, dtype, stream):
@@ -530,7 +554,7 @@ def _new(like, shape, dtype, stream):
     in use by work that waits there, and is handed out again as soon as its tensor goes.)"""
     if stream is None:
         return like.new_empty(shape, dtype=dtype)
-    with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream_of(stream, like), like.device)):
+    with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_handle(stream), like.device)):
         return like.new_empty(shape, dtype=dtype)
 
 
@@ -574,11 +598,12 @@ def wpsgd_quantize(X: Matrix, rows: Optional[torch.Tensor] = None, transpose=Fal
     cm = X.c_struct()
     n, picked = X.m, None
     if rows is not None:
-        assert rows.is_cuda and rows.dtype == torch.int64 and rows.is_contiguous()
+        assert rows.dtype == torch.int64 and rows.is_contiguous()
         n, picked = rows.numel(), rows.data_ptr()
     r, c = (X.d, n) if transpose else (n, X.d)
     blocks = -(-c // 128)
     source = X.dense if X.dense is not None else X.vals
+    index = _beside(source, rows, codes, exps)
     new = codes is None and exps is None
     if codes is None:
         codes = _new(source, (r, 128 * blocks), torch.float8_e4m3fn, stream)
@@ -586,7 +611,7 @@ def wpsgd_quantize(X: Matrix, rows: Optional[torch.Tensor] = None, transpose=Fal
         exps = _new(source, (r, (blocks + 3) // 4 * 4), torch.uint8, stream)
     out = BlockMatrix(r, c, codes, exps)
     c_out = _CBlocks(r, c, codes.data_ptr(), 128 * blocks, exps.data_ptr(), (blocks + 3) // 4 * 4) if new else out.c_struct()
-    rc = load().wpsgd_quantize(ctypes.byref(cm), picked, n, 1 if transpose else 0, ctypes.byref(c_out), _stream_of(stream, source))
+    rc = _call(load().wpsgd_quantize, index, stream, ctypes.byref(cm), picked, n, 1 if transpose else 0, ctypes.byref(c_out))
     if rc != OK:
         raise WpsgdError(rc, "wpsgd_quantize")
     return out
@@ -600,13 +625,14 @@ def wpsgd_block_matmul(A: BlockMatrix, B: BlockMatrix, out: Optional[torch.Tenso
                        workspace: Optional[torch.Tensor] = None, stream=None, fp32_sums=False) -> torch.Tensor:
     """out[i, j] = sum_c A[i, c] B[j, c], float32 or bfloat16.  fp32_sums: bfloat16 results of fp32 sums at large sizes, too, where the 8-bit
     matrix instructions would otherwise drop products under 2^-14 of the largest of their 64."""
+    index = _beside(A.codes, A.exps, B.codes, B.exps, out, workspace)
     if out is None:
         out = _new(A.codes, (A.rows, B.rows), dtype, stream)
-    assert out.is_cuda and out.dtype in _DTYPES and out.shape == (A.rows, B.rows) and (out.numel() == 0 or out.stride(1) == 1)
+    assert out.dtype in _DTYPES and out.shape == (A.rows, B.rows) and (out.numel() == 0 or out.stride(1) == 1)
     L = load()
     p, size, held = _call_workspace(workspace, L.wpsgd_block_matmul_workspace(A.rows, B.rows, A.cols), out, stream)
-    rc = L.wpsgd_block_matmul(ctypes.byref(A.c_struct()), ctypes.byref(B.c_struct()), out.data_ptr(), out.stride(0) if A.rows > 1 else max(out.stride(0), B.rows),
-                              _DTYPES[out.dtype] | (FP32_SUMS if fp32_sums else 0), p, size, _stream_of(stream, out))
+    rc = _call(L.wpsgd_block_matmul, index, stream, ctypes.byref(A.c_struct()), ctypes.byref(B.c_struct()), out.data_ptr(),
+               out.stride(0) if A.rows > 1 else max(out.stride(0), B.rows), _DTYPES[out.dtype] | (FP32_SUMS if fp32_sums else 0), p, size)
     if rc != OK:
         raise WpsgdError(rc, "wpsgd_block_matmul")
     return out
@@ -624,24 +650,24 @@ def wpsgd_softmax_loss(Z: torch.Tensor, labels: torch.Tensor, scale=1.0, row_wei
     """(loss, grad): the rows' weighted cross-entropies (float32) and the gradient of scale * sum(loss) with respect to
     the scores Z, in Z's type.  grad: True for a new tensor, a tensor to write (Z itself too), or False for none."""
     n, c, ld = _rows_of(Z)
-    assert labels.is_cuda and labels.dtype == torch.int64 and labels.is_contiguous() and labels.numel() == n
+    index = _beside(Z, labels, row_weights, loss)
+    assert labels.dtype == torch.int64 and labels.is_contiguous() and labels.numel() == n
     if row_weights is not None:
-        assert row_weights.is_cuda and row_weights.dtype == torch.float32 and row_weights.is_contiguous() and row_weights.numel() == n
+        assert row_weights.dtype == torch.float32 and row_weights.is_contiguous() and row_weights.numel() == n
     if loss is None:
         loss = _new(Z, n, torch.float32, stream)
-    assert loss.is_cuda and loss.dtype == torch.float32 and loss.is_contiguous() and loss.numel() == n
+    assert loss.dtype == torch.float32 and loss.is_contiguous() and loss.numel() == n
     if grad is True:
         grad = _new(Z, (n, c), Z.dtype, stream)
         g_ptr, g_ld = grad.data_ptr(), c
     elif grad is not False and grad is not None:
         gn, gc, g_ld = _rows_of(grad)
-        assert grad.dtype == Z.dtype and gn == n and gc == c
+        assert grad.dtype == Z.dtype and gn == n and gc == c and grad.get_device() == index
         g_ptr = grad.data_ptr()
     else:
         grad, g_ptr, g_ld = None, None, 0
-    rc = load().wpsgd_softmax_loss(Z.data_ptr(), n, c, ld, _DTYPES[Z.dtype], labels.data_ptr(),
-                                   row_weights.data_ptr() if row_weights is not None else None, float(scale), loss.data_ptr(), g_ptr, g_ld,
-                                   _stream_of(stream, Z))
+    rc = _call(load().wpsgd_softmax_loss, index, stream, Z.data_ptr(), n, c, ld, _DTYPES[Z.dtype], labels.data_ptr(),
+               row_weights.data_ptr() if row_weights is not None else None, float(scale), loss.data_ptr(), g_ptr, g_ld)
     if rc != OK:
         raise WpsgdError(rc, "wpsgd_softmax_loss")
     return loss, grad
@@ -672,7 +698,7 @@ def wpsgd_tensor_list(grads, weights=None, stream=None) -> TensorList:
     need = L.wpsgd_tensor_list_bytes(items, len(grads))
     table = _new(grads[0] if grads else torch.empty(0, device=device), need, torch.uint8, stream)
     c_list = _CTensorList()
-    rc = L.wpsgd_tensor_list_make(items, len(grads), table.data_ptr(), table.numel(), ctypes.byref(c_list), _stream(stream))
+    rc = _call(L.wpsgd_tensor_list_make, table.get_device(), stream, items, len(grads), table.data_ptr(), table.numel(), ctypes.byref(c_list))
     if rc != OK:
         raise WpsgdError(rc, "wpsgd_tensor_list_make")
     return TensorList(grads, weights, table, c_list)
@@ -684,12 +710,13 @@ def wpsgd_grad_norm_workspace(tensors: TensorList) -> int:
 
 def _norm_call(name, tensors, args, norm, workspace, stream):
     L = load()
+    index = _beside(tensors.table, norm, workspace)
     if norm is None:
         norm = _new(tensors.table, (), torch.float32, stream)
-    assert norm.is_cuda and norm.dtype == torch.float32 and norm.numel() == 1
+    assert norm.dtype == torch.float32 and norm.numel() == 1
     c_list = ctypes.byref(tensors.c_list)
     p, size, held = _call_workspace(workspace, L.wpsgd_grad_norm_workspace(c_list), norm, stream)
-    rc = getattr(L, name)(c_list, *args, norm.data_ptr(), p, size, _stream_of(stream, norm))
+    rc = _call(getattr(L, name), index, stream, c_list, *args, norm.data_ptr(), p, size)
     if rc != OK:
         raise WpsgdError(rc, name)
     return norm
@@ -717,12 +744,13 @@ def wpsgd_draw_classes(Z: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=
     """(drawn, probs): a class for each row of the scores Z (int64, -1 where none can be drawn) and its probability among
     the classes that were kept (float32).  u: float32 in [0, 1).  Each setting is a number, or a tensor with one for each row (float32; top_k int32)."""
     n, c, ld = _rows_of(Z)
-    assert u.is_cuda and u.dtype == torch.float32 and u.is_contiguous() and u.numel() == n
+    index = _beside(Z, u, drawn, probs)
+    assert u.dtype == torch.float32 and u.is_contiguous() and u.numel() == n
     rule = _CDrawRule(1.0, 0, 1.0, 0.0)
     for name, v, dt in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32),
                         ("min_p", min_p, torch.float32)):
         if isinstance(v, torch.Tensor):
-            assert v.is_cuda and v.dtype == dt and v.is_contiguous() and v.numel() == n
+            assert v.get_device() == index and v.dtype == dt and v.is_contiguous() and v.numel() == n
             setattr(rule, "row_" + name, v.data_ptr())
         else:
             setattr(rule, name, v)
@@ -730,10 +758,9 @@ def wpsgd_draw_classes(Z: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=
         drawn = _new(u, n, torch.int64, stream)
     if probs is None:
         probs = _new(u, n, torch.float32, stream)
-    assert drawn.is_cuda and drawn.dtype == torch.int64 and drawn.is_contiguous() and drawn.numel() == n
-    assert probs.is_cuda and probs.dtype == torch.float32 and probs.is_contiguous() and probs.numel() == n
-    rc = load().wpsgd_draw_classes(Z.data_ptr(), n, c, ld, _DTYPES[Z.dtype], u.data_ptr(), ctypes.byref(rule), drawn.data_ptr(), probs.data_ptr(),
-                                   _stream_of(stream, Z))
+    assert drawn.dtype == torch.int64 and drawn.is_contiguous() and drawn.numel() == n
+    assert probs.dtype == torch.float32 and probs.is_contiguous() and probs.numel() == n
+    rc = _call(load().wpsgd_draw_classes, index, stream, Z.data_ptr(), n, c, ld, _DTYPES[Z.dtype], u.data_ptr(), ctypes.byref(rule), drawn.data_ptr(), probs.data_ptr())
     if rc != OK:
         raise WpsgdError(rc, "wpsgd_draw_classes")
     return drawn, probs

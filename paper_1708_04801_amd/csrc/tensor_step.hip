@@ -13,8 +13,10 @@
 
 namespace wpsgd {
 
-// Elements of a chunk.  A small model in small chunks, so that it spreads over the chip (3M elements: the norm 7.0 us with
-// 16384 to a chunk, 4.7 with 2048; the step 9.3 with either); a large one in large ones, of which a workgroup has many and asks for several vectors at a time.
+// Elements of a chunk.  A small model in small chunks, so that it spreads over the chip; a large one in large ones, of which a workgroup asks for several vectors at a
+// time (a small chunk of bfloat16 has one for each thread).  So an element of bfloat16 counts as four.  us for the norm and for the whole step, 2048 | 16384 to a chunk, out of the caches:
+// fp32 1M 8.1, 7.8 | 8.3, 12.1; 3M 7.5, 13.6 | 8.5, 17.9; 8M 11.4, 28.8 | 13.1, 28.4; 12M 14.1, 39.7 | 14.8, 39.3; 128M 90.6, 391 | 86.9, 386;
+// bfloat16 1M 7.3, 7.8 | 7.4, 8.7; 2M 7.2, 10.0 | 7.4, 9.5; 3M 7.5, 12.0 | 7.5, 10.5; 8M 9.9, 27.2 | 7.2, 22.7; 128M 87.1, 331 | 45.4, 286.
 constexpr int kLargeChunk = 16384, kSmallChunk = 2048;
 constexpr int64_t kSmallModel = 8 << 20;
 constexpr int kNormGroups = 1024;        // partial sums at most, one per workgroup
@@ -201,17 +203,19 @@ static hipError_t launch_square_sums(const wpsgd_tensor_list *l, double *partial
     return hipGetLastError();
 }
 
-static int64_t chunk_of(int64_t elements) { return elements <= kSmallModel ? kSmallChunk : kLargeChunk; }
+static int64_t chunk_of(int64_t counted) { return counted <= kSmallModel ? kSmallChunk : kLargeChunk; }
+static int64_t counted_of(const wpsgd_tensor &t) { return t.dtype == WPSGD_BF16 ? 4 * t.n : t.n; }
 // -1 for descriptions that cannot be
 static int64_t count_chunks(const wpsgd_tensor *tensors, int64_t count)
 {
     if (count < 0 || (count > 0 && !tensors)) return -1;
-    int64_t elements = 0, chunks = 0;
+    int64_t elements = 0, counted = 0, chunks = 0;
     for (int64_t i = 0; i < count; ++i) {
         if (tensors[i].n < 0 || tensors[i].n > (1LL << 44) || elements > (1LL << 44)) return -1;
         elements += tensors[i].n;
+        counted += counted_of(tensors[i]);
     }
-    for (int64_t i = 0; i < count; ++i) chunks += (tensors[i].n + chunk_of(elements) - 1) / chunk_of(elements);
+    for (int64_t i = 0; i < count; ++i) chunks += (tensors[i].n + chunk_of(counted) - 1) / chunk_of(counted);
     return chunks;
 }
 
@@ -235,7 +239,7 @@ int wpsgd_tensor_list_make(const wpsgd_tensor *tensors, int64_t count, void *tab
     if (chunks < 0 || !list || !table || (uintptr_t)table % 256 != 0) return WPSGD_INVALID_ARG;
     if (table_bytes < wpsgd_tensor_list_bytes(tensors, count)) return WPSGD_WORKSPACE_TOO_SMALL;
     bool weights = true;
-    int64_t elements = 0;
+    int64_t elements = 0, counted = 0;
     for (int64_t i = 0; i < count; ++i) {
         const wpsgd_tensor &t = tensors[i];
         if (t.dtype != WPSGD_F32 && t.dtype != WPSGD_BF16) return WPSGD_INVALID_ARG;
@@ -243,9 +247,10 @@ int wpsgd_tensor_list_make(const wpsgd_tensor *tensors, int64_t count, void *tab
         if (!t.grad || (uintptr_t)t.grad % (t.dtype == WPSGD_F32 ? 4 : 2) != 0 || (uintptr_t)t.weight % 4 != 0) return WPSGD_INVALID_ARG;
         weights = weights && t.weight;
         elements += t.n;
+        counted += counted_of(t);
     }
     try {
-        const int64_t each = chunk_of(elements);
+        const int64_t each = chunk_of(counted);
         std::vector<Chunk> host;
         host.reserve((size_t)chunks);
         for (int64_t i = 0; i < count; ++i) {

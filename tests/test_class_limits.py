@@ -18,3 +18,16 @@ def test_products_of_more_workgroups_than_a_launch_has(rows_a, rows_b, dtype):
 def test_products_of_wide_rows_on_both_sides():
     a, b = (api._CBlocks(5_000_000, 128, GB, (1 << 22) + 16, GB, 4) for _ in range(2))
     assert api.load().wpsgd_block_matmul(ctypes.byref(a), ctypes.byref(b), GB, 5_000_000, api.F32, None, 0, None) == api.UNSUPPORTED
+
+
+def test_tables_of_models_on_both_sides_of_the_large_ones():
+    """32 bytes to a chunk: 2048 elements to one up to 8 Mi elements, one of bfloat16 counting as four, and 16384 behind that"""
+    def table(*tensors):
+        items = (api._CTensor * len(tensors))(*(api._CTensor(GB, GB, n, t) for n, t in tensors))
+        return api.load().wpsgd_tensor_list_bytes(items, len(tensors))
+
+    up = lambda chunks: (chunks * 32 + 255) // 256 * 256  # noqa: E731
+    m = 1 << 20
+    assert table((8 * m, api.F32)) == up(8 * m // 2048) and table((8 * m + 1, api.F32)) == up(8 * m // 16384 + 1)
+    assert table((2 * m, api.BF16)) == up(2 * m // 2048) and table((2 * m + 1, api.BF16)) == up(2 * m // 16384 + 1)
+    assert table((4 * m, api.F32), (m, api.BF16)) == up(5 * m // 2048) and table((4 * m + 1, api.F32), (m, api.BF16)) == up(5 * m // 16384 + 1)

@@ -910,8 +910,9 @@ __global__ __launch_bounds__(NT) void draw_row_kernel(DrawArgs a)
 template <typename T>
 static hipError_t launch_draw(DrawArgs a, hipStream_t s)
 {
-    // short rows: four waves, whose barriers are shorter, and several workgroups to a compute unit (us a call with top_p 0.9, four waves | sixteen, bfloat16: 200 rows of
-    // 8000 16.4 | 20.8, one of 16000 17.5 | 21.4, but fp32, 200 of 16000 28.8 | 22.8, and with top 50 13.4 | 11.2)
+    // Short rows: four waves, whose barriers are shorter, and several workgroups to a compute unit.  us a call, four waves | sixteen, bfloat16 and fp32:
+    //   8192 classes, 200 rows   top_p 0.9 16.1 | 18.8, 16.7 | 17.8    top 50 10.4 | 8.9, 12.1 | 8.8     1000 rows  top_p 0.9 31 | 68, 33 | 67    top 50 19 | 31, 21 | 32
+    //   16384 classes, 200 rows  top_p 0.9 19.8 | 21.1, 29.0 | 19.9    top_p 0.5, whose list has no room in the smaller LDS, 54 | 21, 83 | 19
     const bool few = a.c <= 8192;
     return in_launches(a.n, few ? 256 : 1024, [&](int64_t first, unsigned count) {
         a.first = first;

@@ -53,7 +53,7 @@ __device__ inline void store4(uint16_t *p, const f32x4 &v)
 // Few rows against many.  The one operand's rows (the class vectors of a serving call) are read once, straight from memory into the matrix instructions, sixteen
 // rows times NT to a wave; the other's 16 MT rows lie in LDS as bfloat16 fragments, a few blocks of the sum at a time (asked for by each wave
 // they are a trip to the L2 a block: 16 x 65536 x 4096 79 us, 64 x 65536 x 4096 138).  kRowWaves waves to a workgroup: `along` of them share the blocks of the
-// sum in turn and add up through LDS, in their order, the others take the next rows.  Bound by memory: 16 x 65536 x 4096 reads 270 MB in 62 to 64 us, 4.2 TB/s and more; 1 x 4096 x
+// sum in turn and add up through LDS, in their order, the others take the next rows.  Bound by memory: 16 x 65536 x 4096 reads 270 MB out of the caches in 66 us, 4.1 TB/s; 1 x 4096 x
 // 4096, 17 MB in 8.6 us, is a start and a few trips.
 // `turned`: the many rows are A's (results of a lane lie below each other), else B's (beside each other).
 constexpr int kRowWaves = 8;
@@ -632,7 +632,7 @@ template <typename TO>
 static hipError_t launch_rows(const MatmulArgs &g, hipStream_t s)
 {
     const RowsShape r = rows_shape(g.M, g.N);
-    if (r.mt == 1) return r.nt == 2 ? launch_rows_of<1, 2, TO>(g, r.turned, s) : launch_rows_of<1, 1, TO>(g, r.turned, s);
+    if (r.mt == 1) return launch_rows_of<1, 1, TO>(g, r.turned, s);
     if (r.mt == 2) return r.nt == 2 ? launch_rows_of<2, 2, TO>(g, r.turned, s) : launch_rows_of<2, 1, TO>(g, r.turned, s);
     return r.nt == 2 ? launch_rows_of<4, 2, TO>(g, r.turned, s) : launch_rows_of<4, 1, TO>(g, r.turned, s);
 }

@@ -43,7 +43,11 @@ inline RowsShape rows_shape(int64_t M, int64_t N)
     const bool turned = M > N;
     const int64_t many = turned ? M : N, few = turned ? N : M;
     // too few rows for the compute units: the few rows in sixteens beside each other, too (64 x 1000 x 4096: 28 us without that)
-    return {few <= 16 || many <= 2048 ? 1 : few <= 32 ? 2 : 4, many >= 32 * 2048 ? 2 : 1, turned};
+    const int mt = few <= 16 || many <= 2048 ? 1 : few <= 32 ? 2 : 4;
+    // Two sixteens of the many share what is read of the few from LDS, and leave half the waves. us, one | two, sums of 4096, the many out of the caches:
+    //   16 x 65536 66 | 71, x 131072 124 | 130, x 262144 243 | 251      32 x 65536 73 | 77, x 98304 108 | 123, x 131072 142 | 140, x 262144 273 | 261
+    //   64 x 49152 84 | 88, x 65536 90 | 85, x 98304 134 | 140, x 131072 174 | 154, x 262144 333 | 291
+    return {mt, mt > 1 && many * mt >= 1 << 18 ? 2 : 1, turned};
 }
 
 // rows of a tile are addressed with 32 bits

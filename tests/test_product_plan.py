@@ -40,7 +40,7 @@ def test_few_rows(plan):
         for f32 in (F32, BF16):
             p = plan(m, n, k, f32)
             assert p["kind"] == "rows" and p["sixteens"] == sixteens and p["turned"] == (m > n), (m, n, k)
-    assert {s[3] for s in shapes.ROWS} == {(a, b) for a in (1, 2, 4) for b in (1, 2)}
+    assert {s[3] for s in shapes.ROWS} == {(1, 1), (2, 1), (2, 2), (4, 1), (4, 2)}
     assert all({plan(m, n, k, F32)["turned"] for m, n, k, s in shapes.ROWS if s[1] == nt} == {True, False} for nt in (1, 2))
 
 

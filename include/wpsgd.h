@@ -388,8 +388,8 @@ int wpsgd_clipped_step(const wpsgd_tensor_list *list, double eta, double lambda,
  * counts as -inf, and -inf is never drawn).  Kept are the first top_k (<= 0: all), of those the ones whose weight is at
  * least min_p times the largest, and of those the shortest run from the front that holds top_p of their weight (>= 1: all;
  * at least one class).  With q_c = floor(2^((z_c - max) * log2(e) / temperature) * 2^31 + 1/2) and Q the sum over what is kept, the
- * answer is the first kept class, by index, at which the sum of q passes floor(u * Q).  Weights and sums are whole numbers: the same row gets the
- * same answer however many rows or compute units a call has.  temperature 0: the largest score (lowest index).
+ * answer is the first kept class, by index, at which the sum of q passes floor(u * Q).  The power of two is fp32's, off by up to 5e-6 of itself; weights and
+ * sums are whole numbers: the same row gets the same answer however many rows or compute units a call has.  temperature 0: the largest score (lowest index).
  * A field row_x, DEVICE with n entries, stands in for x where it is not NULL.                                           */
 typedef struct wpsgd_draw_rule {
     float temperature;

@@ -2,9 +2,9 @@
 //
 // Classes stand in order of score, the lower index first among equals; -inf and NaN cannot be drawn.  What may be drawn is a run from the front of that
 // order: the first top_k, of those the ones whose weight is at least min_p of the largest, and of those the shortest run that holds top_p of their weight.
-// Weights are whole numbers, q = floor(2^((x - max) log2e / T) 2^31 + 1/2), and their sums 64-bit integers: no sum depends on the order it is taken
-// in, so neither does a draw, and a weight is off by 2^-32 of the largest at most.  The run's end is found digit by digit on the
-// scores' bits (four digits of eight bits, the counts or weights of each in LDS), and the draw walks the kept classes by index.
+// Weights are whole numbers, q = floor(2^((x - max) log2e / T) 2^31 + 1/2), the power of two in fp32 (off by up to 5e-6 of itself), and their sums 64-bit integers: no sum
+// depends on the order it is taken in, so neither does a draw.  Few kept classes go to a list in LDS, where everything else is done; else the run's end is guessed from a sample, looked
+// for in a list of what lies near it, and digit by digit among all scores only where that fails; the draw walks the kept classes by index.
 #include <cmath>
 #include <type_traits>
 

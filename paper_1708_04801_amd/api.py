@@ -596,21 +596,23 @@ def wpsgd_quantize(X: Matrix, rows: Optional[torch.Tensor] = None, transpose=Fal
     """Rows of a dense data set (all, or those that `rows`, int64 on the GPU, names) as a BlockMatrix, blocks along the
     columns; transpose=True: one row for each column of X, blocks along the rows taken."""
     cm = X.c_struct()
-    n, picked = X.m, None
+    source = X.dense if X.dense is not None else X.vals
+    n, picked, index = X.m, None, source.get_device()
     if rows is not None:
-        assert rows.dtype == torch.int64 and rows.is_contiguous()
+        assert rows.dtype == torch.int64 and rows.is_contiguous() and rows.get_device() == index
         n, picked = rows.numel(), rows.data_ptr()
     r, c = (X.d, n) if transpose else (n, X.d)
     blocks = -(-c // 128)
-    source = X.dense if X.dense is not None else X.vals
-    index = _beside(source, rows, codes, exps)
-    new = codes is None and exps is None
-    if codes is None:
-        codes = _new(source, (r, 128 * blocks), torch.float8_e4m3fn, stream)
-    if exps is None:
-        exps = _new(source, (r, (blocks + 3) // 4 * 4), torch.uint8, stream)
-    out = BlockMatrix(r, c, codes, exps)
-    c_out = _CBlocks(r, c, codes.data_ptr(), 128 * blocks, exps.data_ptr(), (blocks + 3) // 4 * 4) if new else out.c_struct()
+    words = (blocks + 3) // 4 * 4
+    if codes is None and exps is None:
+        codes, exps = _new(source, (r, 128 * blocks), torch.float8_e4m3fn, stream), _new(source, (r, words), torch.uint8, stream)
+        out = BlockMatrix(r, c, codes, exps)
+        c_out = _CBlocks(r, c, codes.data_ptr(), 128 * blocks, exps.data_ptr(), words)
+    else:
+        _beside(source, codes, exps)
+        out = BlockMatrix(r, c, codes if codes is not None else _new(source, (r, 128 * blocks), torch.float8_e4m3fn, stream),
+                          exps if exps is not None else _new(source, (r, words), torch.uint8, stream))
+        c_out = out.c_struct()
     rc = _call(load().wpsgd_quantize, index, stream, ctypes.byref(cm), picked, n, 1 if transpose else 0, ctypes.byref(c_out))
     if rc != OK:
         raise WpsgdError(rc, "wpsgd_quantize")
@@ -628,7 +630,9 @@ def wpsgd_block_matmul(A: BlockMatrix, B: BlockMatrix, out: Optional[torch.Tenso
     index = _beside(A.codes, A.exps, B.codes, B.exps, out, workspace)
     if out is None:
         out = _new(A.codes, (A.rows, B.rows), dtype, stream)
-    assert out.dtype in _DTYPES and out.shape == (A.rows, B.rows) and (out.numel() == 0 or out.stride(1) == 1)
+        assert dtype in _DTYPES
+    else:
+        assert out.dtype in _DTYPES and out.shape == (A.rows, B.rows) and (out.numel() == 0 or out.stride(1) == 1)
     L = load()
     p, size, held = _call_workspace(workspace, L.wpsgd_block_matmul_workspace(A.rows, B.rows, A.cols), out, stream)
     rc = _call(L.wpsgd_block_matmul, index, stream, ctypes.byref(A.c_struct()), ctypes.byref(B.c_struct()), out.data_ptr(),
@@ -656,7 +660,8 @@ def wpsgd_softmax_loss(Z: torch.Tensor, labels: torch.Tensor, scale=1.0, row_wei
         assert row_weights.dtype == torch.float32 and row_weights.is_contiguous() and row_weights.numel() == n
     if loss is None:
         loss = _new(Z, n, torch.float32, stream)
-    assert loss.dtype == torch.float32 and loss.is_contiguous() and loss.numel() == n
+    else:
+        assert loss.dtype == torch.float32 and loss.is_contiguous() and loss.numel() == n
     if grad is True:
         grad = _new(Z, (n, c), Z.dtype, stream)
         g_ptr, g_ld = grad.data_ptr(), c
@@ -713,7 +718,8 @@ def _norm_call(name, tensors, args, norm, workspace, stream):
     index = _beside(tensors.table, norm, workspace)
     if norm is None:
         norm = _new(tensors.table, (), torch.float32, stream)
-    assert norm.dtype == torch.float32 and norm.numel() == 1
+    else:
+        assert norm.dtype == torch.float32 and norm.numel() == 1
     c_list = ctypes.byref(tensors.c_list)
     p, size, held = _call_workspace(workspace, L.wpsgd_grad_norm_workspace(c_list), norm, stream)
     rc = _call(getattr(L, name), index, stream, c_list, *args, norm.data_ptr(), p, size)
@@ -756,10 +762,12 @@ def wpsgd_draw_classes(Z: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=
             setattr(rule, name, v)
     if drawn is None:
         drawn = _new(u, n, torch.int64, stream)
+    else:
+        assert drawn.dtype == torch.int64 and drawn.is_contiguous() and drawn.numel() == n
     if probs is None:
         probs = _new(u, n, torch.float32, stream)
-    assert drawn.dtype == torch.int64 and drawn.is_contiguous() and drawn.numel() == n
-    assert probs.dtype == torch.float32 and probs.is_contiguous() and probs.numel() == n
+    else:
+        assert probs.dtype == torch.float32 and probs.is_contiguous() and probs.numel() == n
     rc = _call(load().wpsgd_draw_classes, index, stream, Z.data_ptr(), n, c, ld, _DTYPES[Z.dtype], u.data_ptr(), ctypes.byref(rule), drawn.data_ptr(), probs.data_ptr())
     if rc != OK:
         raise WpsgdError(rc, "wpsgd_draw_classes")

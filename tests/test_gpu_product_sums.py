@@ -11,7 +11,7 @@ from test_gpu_product_kernels import blocks, gen, values, whole
 pytestmark = pytest.mark.gpu
 
 
-@pytest.mark.parametrize("m,n,k", [*shapes.FAST_256, *shapes.TILES_256, (129, 257, 520), (5, 3001, 129), (200, 200, 65536)])
+@pytest.mark.parametrize("m,n,k", [*shapes.FAST_256, *shapes.TILES_256, *shapes.SUMS_256, (129, 257, 520), (5, 3001, 129), (200, 200, 65536)])
 def test_small_products_beside_large_ones_that_cancel(m, n, k):
     """a pair of products 2^16 and -2^16 in every block, and whole numbers up to 16 beside them: exact in fp32"""
     g = gen(m, n, k, 7)
@@ -27,7 +27,7 @@ def test_small_products_beside_large_ones_that_cancel(m, n, k):
     assert torch.equal(exact, want.float())
 
 
-@pytest.mark.parametrize("m,n,k", shapes.FAST_256 + shapes.TILES_256[2:6])
+@pytest.mark.parametrize("m,n,k", shapes.FAST_256 + shapes.TILES_256[2:6] + shapes.SUMS_256)
 def test_random_rows(m, n, k):
     """the bound of fp32 sums (sqrt(K) roundings by 2^-24 of |a| |b|, six standard deviations) and half of bfloat16's last place"""
     g = gen(m, n, k, 8)

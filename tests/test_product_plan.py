@@ -77,5 +77,7 @@ def test_wide_rows_go_where_addresses_are_64_bits(plan):
 def test_sums_asked_for(plan):
     for m, n, k in shapes.FAST_256:
         assert plan(m, n, k, BF16, sums=True)["kind"] in ("tile128", "tile256")
+    for m, n, k in shapes.SUMS_256:
+        assert plan(m, n, k, BF16, sums=True)["kind"] == "tile256"
     for m, n, k in shapes.TILES_256:
         assert plan(m, n, k, F32, sums=True) == plan(m, n, k, F32) and plan(m, n, k, BF16, sums=True)["kind"] == "tile256"

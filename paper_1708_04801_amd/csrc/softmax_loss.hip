@@ -12,7 +12,7 @@ struct LossArgs {
     int64_t n, c, ld;
     const int64_t *labels;
     const float *row_weights;
-    float scale;
+    double scale;
     float *loss;
     void *grad;
     int64_t ld_grad;
@@ -132,7 +132,7 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void softmax_row_kernel(LossAr
     const float bad = label >= a.c ? __builtin_nanf("") : 0.0f;                   // no such class: loss and gradient say so
     if (t == 0) a.loss[row] = label >= a.c ? bad : empty ? kInf : (m - z_label + logf(s)) * r;
     if (!g) return;
-    const float f = a.scale * r, over = (empty ? 0.0f : f / s) + bad;
+    const float f = (float)(a.scale * (double)r), over = (empty ? 0.0f : f / s) + bad;
     const int at_label = empty || label >= a.c ? -1 : (int)label;
     auto gradient = [&](int v, const Bytes16 &x, auto kept) {
         float p[E];
@@ -198,7 +198,7 @@ int wpsgd_softmax_loss(const void *Z, int64_t n, int64_t classes, int64_t ld, wp
     if (grad && (ld_grad < classes || (uintptr_t)grad % elem != 0)) return WPSGD_INVALID_ARG;
     if (grad == Z && ld_grad != ld) return WPSGD_INVALID_ARG;
     if (!(scale - scale == 0.0)) return WPSGD_INVALID_ARG;
-    const LossArgs a{Z, n, classes, ld, labels, row_weights, (float)scale, loss, grad, ld_grad, 0};
+    const LossArgs a{Z, n, classes, ld, labels, row_weights, scale, loss, grad, ld_grad, 0};
     hipStream_t s = static_cast<hipStream_t>(stream);
     const hipError_t e = dtype == WPSGD_F32 ? launch_loss<float>(a, s) : launch_loss<uint16_t>(a, s);
     return e == hipSuccess ? WPSGD_OK : hip_fail(e);

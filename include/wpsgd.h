@@ -340,7 +340,8 @@ int wpsgd_block_matmul(const wpsgd_blocks *A, const wpsgd_blocks *B, void *out, 
  *   loss[i]    = r_i * (log sum_c exp(z_ic) - z_i,label)
  *   grad[i, c] = scale * r_i * (softmax(z_i)_c - [c = label_i])          the gradient of scale * sum_i loss[i]
  * A row with a negative label or r_i = 0 does not count: loss and gradient are 0 whatever its scores.  A row whose scores
- * are all -inf has loss +inf and gradient 0.  A label >= classes makes the row's loss and gradient NaN.
+ * are all -inf has loss +inf and gradient 0.  A label >= classes makes the row's loss and gradient NaN, and so does a score of a row
+ * that counts which is +inf or NaN.
  *   Z            DEVICE, n x classes, row stride ld elements, fp32 or bfloat16
  *   labels       DEVICE, n                    row_weights  DEVICE, n (r_i), or NULL for ones
  *   loss         DEVICE out, n fp32           grad         DEVICE out, dtype as Z, row stride ld_grad; NULL: not wanted.
@@ -403,7 +404,8 @@ typedef struct wpsgd_draw_rule {
  *   u        DEVICE, n numbers in [0, 1)
  *   drawn    DEVICE out, n; -1 for a row without a class that can be drawn
  *   probs    DEVICE out, n, or NULL: q / Q of the class drawn (0 beside -1)
- * A row's setting cannot be refused: a temperature that is no positive number counts as 0, a min_p over 1 or NaN as 1.
+ * A row's setting cannot be refused: a temperature that is no positive number counts as 0, a min_p over 1 or NaN as 1, a top_p
+ * that is NaN as 1.
  * Errors: INVALID_ARG (temperature >= 0, min_p <= 1, neither NaN, nor top_p), UNSUPPORTED, HIP_ERROR.                  */
 int wpsgd_draw_classes(const void *Z, int64_t n, int64_t classes, int64_t ld, wpsgd_dtype dtype, const float *u,
                        const wpsgd_draw_rule *rule, int64_t *drawn, float *probs, void *stream);

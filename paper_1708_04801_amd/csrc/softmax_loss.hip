@@ -23,7 +23,7 @@ constexpr float kLog2e = 1.44269504088896340736f, kLog2eRest = 1.92596299e-8f;  
 // e^x for x <= 0.  For fp32 rows to a last place or two, subnormal results too, since their gradient keeps it: with x log2 e rounded once the gradient of a class 100 under the largest is
 // off by 7e-6 of itself.  x log2 e = n + f with f exact but for its own rounding; n is held at -300, so that -inf comes out as 2^-inf and a NaN as itself.  The row's sum and its
 // gradient share the exponential: 4096 x 65536 fp32 with the gradient 414 us, 408 with the short form (loss alone 220 | 187; up to 32000 classes no difference).
-// bfloat16 gradients round to 2^-8, and the short form is off by |x| 2^-23, least in the terms that make up the row's sum.
+// bfloat16 gradients round to 2^-8, and the short form is off by |x| 2^-23, least in the terms that make up the row's sum (and 0 under 2^-126).
 template <typename T> __device__ inline float exp_of(float x)
 {
     if constexpr (Elem<T>::kPer16 == 4) {

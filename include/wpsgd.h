@@ -329,8 +329,8 @@ int wpsgd_quantize(const wpsgd_matrix *X, const int64_t *rows, int64_t n, int tr
  *   out        DEVICE, A->rows x B->rows; it may not overlap A or B
  *   workspace  DEVICE scratch of at least wpsgd_block_matmul_workspace(A->rows, B->rows, A->cols) bytes, 256-byte aligned
  *              (may be NULL where that is 0)
- * The result does not depend on timing.  Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, UNSUPPORTED (2^31 rows or more; row strides over
- * 4 MiB with more than 4 million rows on both sides), HIP_ERROR.                                                       */
+ * The result does not depend on timing.  Errors: INVALID_ARG, WORKSPACE_TOO_SMALL, UNSUPPORTED (2^31 rows or more; more than 64 rows on
+ * both sides and 2^24 tiles of 128 x 128 results or more; row strides over 4 MiB and 4 million rows on both sides), HIP_ERROR. */
 size_t wpsgd_block_matmul_workspace(int64_t rows_a, int64_t rows_b, int64_t cols);
 #define WPSGD_FP32_SUMS 16     /* with the dtype of wpsgd_block_matmul's results */
 int wpsgd_block_matmul(const wpsgd_blocks *A, const wpsgd_blocks *B, void *out, int64_t ld_out, int dtype_and_sums,

@@ -24,6 +24,7 @@ struct MatmulArgs {
     void *out;
     int64_t ldo;
     int each;                  // blocks to a part of the sum (all, where it is not split)
+    int64_t first;             // workgroup of the call at which the launch begins (few rows against many)
 };
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -72,7 +73,7 @@ __global__ __launch_bounds__(64 * kRowWaves) void matmul_rows_kernel(MatmulArgs 
     const int64_t ld_many = turned ? g.lda : g.ldb, ld_few = turned ? g.ldb : g.lda, lde_many = turned ? g.lde_a : g.lde_b, lde_few = turned ? g.lde_b : g.lde_a;
     const int64_t rows_many = turned ? g.M : g.N, rows_few = turned ? g.N : g.M;
     const int across = kRowWaves / along, mine = wave % along;
-    const int64_t s0 = ((int64_t)blockIdx.x * across + wave / along) * (16 * NT), h0 = (int64_t)blockIdx.y * (16 * MT);
+    const int64_t s0 = ((g.first + blockIdx.x) * across + wave / along) * (16 * NT), h0 = (int64_t)blockIdx.y * (16 * MT);
     const int r = lane & 15, group = lane >> 4;
     const bool idle = s0 >= rows_many;
     f32x4 acc[MT][NT];
@@ -617,16 +618,18 @@ __global__ __launch_bounds__(256) void join_parts_kernel(const float *parts, int
 static size_t parts_bytes(const MatmulPlan &p, int64_t M, int64_t N) { return p.parts > 1 ? ((size_t)p.parts * M * N * sizeof(float) + 255) & ~(size_t)255 : 0; }
 
 template <int MT, int NT, typename TO>
-static hipError_t launch_rows_of(const MatmulArgs &g, bool turned, hipStream_t s)
+static hipError_t launch_rows_of(MatmulArgs g, bool turned, hipStream_t s)
 {
     const int64_t many = turned ? g.M : g.N, few = turned ? g.N : g.M;
     const int64_t groups = (many + 16 * NT - 1) / (16 * NT), panels = (few + 16 * MT - 1) / (16 * MT);
     int along = 1;
     while (along < kRowWaves && along < kHeldBlocks / MT && groups * panels * along < 2048 && g.blocks >= 2 * along) along *= 2;
     const int64_t grid = (groups * along + kRowWaves - 1) / kRowWaves;
-    if (grid > most_groups(64 * kRowWaves) || panels > 65535) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((matmul_rows_kernel<MT, NT, TO>), dim3((unsigned)grid, (unsigned)panels), dim3(64 * kRowWaves), 0, s, g, along, turned);
-    return hipGetLastError();
+    if (many >= 1LL << 31 || panels > 65535) return hipErrorInvalidConfiguration;
+    return in_launches(grid, 64 * kRowWaves, [&](int64_t first, unsigned count) {
+        g.first = first;
+        hipLaunchKernelGGL((matmul_rows_kernel<MT, NT, TO>), dim3(count, (unsigned)panels), dim3(64 * kRowWaves), 0, s, g, along, turned);
+    });
 }
 template <typename TO>
 static hipError_t launch_rows(const MatmulArgs &g, hipStream_t s)
@@ -672,14 +675,14 @@ int wpsgd_block_matmul(const wpsgd_blocks *A, const wpsgd_blocks *B, void *out, 
     if (need && (!workspace || (uintptr_t)workspace % 256 != 0)) return WPSGD_INVALID_ARG;
     if (workspace_bytes < need) return WPSGD_WORKSPACE_TOO_SMALL;
     MatmulArgs g{static_cast<const uint8_t *>(A->codes), static_cast<const uint8_t *>(B->codes), static_cast<const uint8_t *>(A->exps),
-                 static_cast<const uint8_t *>(B->exps), A->ld, B->ld, A->ld_exps, B->ld_exps, A->rows, B->rows, (int)((A->cols + 127) / 128), out, ld_out, 0};
+                 static_cast<const uint8_t *>(B->exps), A->ld, B->ld, A->ld_exps, B->ld_exps, A->rows, B->rows, (int)((A->cols + 127) / 128), out, ld_out, 0, 0};
     const bool f32 = dtype == WPSGD_F32;
     const MatmulPlan p = plan_matmul(g.M, g.N, g.blocks, f32, wide(g.lda, g.lde_a) || wide(g.ldb, g.lde_b), sums);
     hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t e = hipSuccess;
     if (p.kind == MatmulPlan::Rows) {
         e = f32 ? launch_rows<float>(g, s) : launch_rows<uint16_t>(g, s);
-        if (e == hipErrorInvalidConfiguration) return WPSGD_UNSUPPORTED;     // more workgroups than a grid has
+        if (e == hipErrorInvalidConfiguration) return WPSGD_UNSUPPORTED;     // more rows than the header takes
     } else {
         const int64_t side = p.kind == MatmulPlan::Tile128 ? 128 : 256;
         const int64_t tiles = ((g.M + side - 1) / side) * ((g.N + side - 1) / side);

@@ -60,3 +60,29 @@ def test_columns_in_blocks():
     for lo, hi in ((0, 5), (GROUPS - 5, GROUPS + 1), (blocks - 3, blocks)):
         one = api.wpsgd_quantize(api.Matrix((hi - lo) * 128, 1, dense=x[lo * 128:hi * 128]), transpose=True)
         assert torch.equal(one.codes.view(torch.uint8), q.codes[:, lo * 128:hi * 128].view(torch.uint8)) and torch.equal(one.exps[:, :hi - lo], q.exps[:, lo:hi])
+
+
+def test_products_of_few_rows():
+    """a thousand million rows of one block against one and against sixteen: 2^23 workgroups of 512 threads and more"""
+    torch.cuda.empty_cache()
+    edge = ((1 << 23) - 1) * 128                      # rows of the first launch
+    n = edge + 1000
+    if torch.cuda.mem_get_info()[0] < n * 170:
+        pytest.skip("not enough memory free for 143 GB of operands and 34 GB of results")
+    codes = torch.zeros((n, 128), dtype=torch.uint8, device="cuda")
+    exps = torch.full((n, 4), 127, dtype=torch.uint8, device="cuda")
+    for lo, hi in places(edge, n):
+        codes[lo:hi] = torch.randint(0, 126, (hi - lo, 128), dtype=torch.uint8, device="cuda")
+    many = api.BlockMatrix(n, 128, codes.view(torch.float8_e4m3fn), exps)
+    for few in (1, 16):
+        x = torch.randn(few, 128, generator=torch.Generator().manual_seed(few)).cuda()
+        a = api.wpsgd_quantize(api.Matrix(few, 128, dense=x))
+        out = torch.full((n, few), 7.0, dtype=torch.bfloat16, device="cuda")
+        api.wpsgd_block_matmul(many, a, out=out)
+        for lo, hi in places(edge, n):
+            part = api.BlockMatrix(hi - lo, 128, codes[lo:hi].view(torch.float8_e4m3fn), exps[lo:hi])
+            want = api.wpsgd_block_matmul(part, a)
+            assert bool(want.any()) and torch.equal(out[lo:hi], want)
+        assert not bool(out[200:edge - 200].any()) and not bool(out[edge + 200:n - 200].any())
+        del out
+    torch.cuda.empty_cache()

@@ -199,15 +199,15 @@ def _own_dropout(s):
 def _own_served(s):
     from paper_1708_04801_amd import api
     X = api.Matrix(s["X"].shape[0], s["X"].shape[1], dense=s["X"])
-    W = api.FourBitMatrix(s["case"]["classes"], s["case"]["d"], s["case"]["group"], s["codes"], s["scales"])
-    return api.wpsgd_matmul4(X, W, rows=s["picked"], dtype=TYPES[s["case"]["out"]])
+    W = api.NibbleMatrix(s["case"]["classes"], s["case"]["d"], s["case"]["group"], s["codes"], s["scales"])
+    return api.wpsgd_nibble_matmul(X, W, rows=s["picked"], dtype=TYPES[s["case"]["out"]])
 
 
 def _own_fresh(s):
     from paper_1708_04801_amd import api
     X = api.Matrix(s["X"].shape[0], s["X"].shape[1], dense=s["X"])
-    W = api.wpsgd_quantize4(api.Matrix(s["W"].shape[0], s["W"].shape[1], dense=s["W"]), group=s["case"]["group"])
-    return api.wpsgd_matmul4(X, W, rows=s["picked"], dtype=TYPES[s["case"]["out"]])
+    W = api.wpsgd_quantize_nibbles(api.Matrix(s["W"].shape[0], s["W"].shape[1], dense=s["W"]), group=s["case"]["group"])
+    return api.wpsgd_nibble_matmul(X, W, rows=s["picked"], dtype=TYPES[s["case"]["out"]])
 
 
 def _softmax(z):

@@ -410,6 +410,89 @@ typedef struct wpsgd_draw_rule {
 int wpsgd_draw_classes(const void *Z, int64_t n, int64_t classes, int64_t ld, wpsgd_dtype dtype, const float *u,
                        const wpsgd_draw_rule *rule, int64_t *drawn, float *probs, void *stream);
 
+/* Clipped policy loss of one drawn class a_i for each row of scores, and its gradient.  With l_i = z_i,a - log sum_c exp(z_ic), ratio_i = exp(l_i - old_log_i) and
+ * A_i = advantage_i:
+ *   loss[i]     = r_i * (-min(ratio_i * A_i, clip(ratio_i, 1 - clip_low, 1 + clip_high) * A_i) + kl * (exp(ref_log_i - l_i) - (ref_log_i - l_i) - 1))
+ *   grad[i, c]  = d (scale * sum_i loss[i]) / d z_ic    (a ratio on a border counts as inside)
+ *   log_prob[i] = l_i
+ * A row with a negative class (wpsgd_draw_classes writes -1) or r_i = 0 does not count: loss, log_prob and gradient are 0 whatever its scores.  A row whose
+ * drawn class has no probability (a score of -inf) has log_prob -inf, a ratio of 0 and a gradient of 0, and so has one whose loss fp32 can only call infinite a
+ * gradient of 0.  An advantage of 0 makes 0 of any ratio, and a ref_log of
+ * -inf beside a log_prob of -inf a KL term of 0.  A class >= classes makes the row's results NaN, and so does a score of a row that counts which is +inf or NaN.
+ *   Z          DEVICE, n x classes, row stride ld elements, fp32 or bfloat16       drawn      DEVICE, n
+ *   old_log    DEVICE, n: log probabilities when the classes were drawn; NULL: these scores' own (ratio 1)
+ *   ref_log    DEVICE, n: log probabilities under a reference; it may be NULL, and is not read, where kl is 0
+ *   advantage  DEVICE, n         row_weights  DEVICE, n (r_i), or NULL for ones
+ *   loss       DEVICE out, n     log_prob     DEVICE out, n, or NULL
+ *   grad       DEVICE out, dtype as Z, row stride ld_grad; NULL: not wanted.  It may be Z itself (with ld_grad = ld), else it may not overlap it.
+ * (All of them fp32 but Z, drawn and grad.)  -loss of wpsgd_softmax_loss without a gradient is a log probability too.  Statistics are fp32, what a row makes of them fp64;
+ * the result does not depend on timing.  Errors: INVALID_ARG (0 <= clip_low <= 1; clip_high >= 0, it may be infinite; kl >= 0), HIP_ERROR. */
+int wpsgd_policy_loss(const void *Z, int64_t n, int64_t classes, int64_t ld, wpsgd_dtype dtype, const int64_t *drawn, const float *old_log,
+                      const float *ref_log, const float *advantage, const float *row_weights, double clip_low, double clip_high, double kl,
+                      double scale, float *loss, float *log_prob, void *grad, int64_t ld_grad, void *stream);
+
+/* Loss of paired log ratios, and its gradient: of each pair of sequences of rows the first is the preferred one.  With l_i the log probability of row i's label,
+ * S_q = the sum over sequence q's rows of r_i * (l_i - ref_log_i), and L the loss `kind` of a margin (HINGE max(0, 1 - h), LOGISTIC log(1 + exp(-h))):
+ *   margin[p]   = h_p = beta * (S_2p - S_2p+1)
+ *   loss[p]     = w_p * ((1 - smoothing) * L(h_p) + smoothing * L(-h_p))
+ *   grad[i, c]  = d (scale * sum_p loss[p]) / d z_ic     (0 for rows that no sequence holds)
+ * Sequence q holds rows offsets[q] .. offsets[q+1]-1 of Z; it may be empty.  A row with a negative label or r_i = 0 does not count, whatever its scores: nothing is
+ * added and its gradient is 0.  A pair with w_p = 0 has loss 0 and gradient 0.  A row whose scores are all -inf has l_i = -inf and gradient 0; l_i - ref_log_i is 0 where
+ * both are -inf.  A label >= classes makes the pair's results NaN, and so does a score of a row that counts which is +inf or NaN.
+ *   Z             DEVICE, n x classes, row stride ld elements, fp32 or bfloat16    labels  DEVICE, n
+ *   offsets       DEVICE, 2 * pairs + 1 row numbers, none under the one before it, within 0 .. n.  Where a pair's are not, its loss and margin are NaN (and the gradient of
+ *                 rows that two pairs then claim is that of either).
+ *   ref_log       DEVICE, n fp32 (-loss of wpsgd_softmax_loss under a reference), or NULL for zeros
+ *   row_weights   DEVICE, n fp32 (r_i), or NULL for ones         pair_weights  DEVICE, pairs fp32 (w_p), or NULL for ones
+ *   loss, margin  DEVICE out, pairs fp32
+ *   grad          DEVICE out, dtype as Z, row stride ld_grad; NULL: not wanted.  It may be Z itself (with ld_grad = ld), else it may not overlap it.
+ *   workspace     DEVICE scratch of at least wpsgd_preference_loss_workspace(n) bytes, 256-byte aligned
+ * Statistics are fp32, sums over rows fp64; the result does not depend on timing.  Errors: INVALID_ARG (0 <= smoothing <= 1), WORKSPACE_TOO_SMALL, HIP_ERROR. */
+size_t wpsgd_preference_loss_workspace(int64_t n);
+int wpsgd_preference_loss(const void *Z, int64_t n, int64_t classes, int64_t ld, wpsgd_dtype dtype, const int64_t *labels, const int64_t *offsets,
+                          int64_t pairs, const float *ref_log, const float *row_weights, const float *pair_weights, wpsgd_loss kind, double beta,
+                          double smoothing, double scale, float *loss, float *margin, void *grad, int64_t ld_grad, void *workspace,
+                          size_t workspace_bytes, void *stream);
+
+/* Rows of X (dense; CSR: UNSUPPORTED) with elements dropped at random and the others scaled:
+ *   out[i*ld_out + c] = 0 where the 16 bits of (seed, chain, step, i, c) are under t = floor(65536 * p + 1/2), else x * 65536 / (65536 - t),
+ * so that an element is dropped with probability t / 65536 and keeps its mean.  The bits are those c % 8 of a Philox4x32-10 block (word c % 8 / 2, its lower half
+ * first) with key seed and counter (c / 8, i, chain, 2^30 + s mod 2^30), s = step + *more_steps: no counter of the sample streams.  The mask is never stored: the gradient
+ * of the rows is the same call on out's gradient (with rows NULL: i counts the rows taken, whichever they are).  What is dropped is 0 whatever it was.
+ *   rows        DEVICE, n row numbers, as for wpsgd_quantize; one outside [0, m) stands for a row of zeros.  NULL: rows 0 .. n-1
+ *   p           0 .. 1                             seed, chain >= 0, step >= 0   as for wpsgd_sample_indices
+ *   more_steps  DEVICE, one number, read when the work runs (so that a replayed graph can go on to other masks), or NULL for 0
+ *   out         DEVICE, n x d of X's dtype.  It may be X itself (rows NULL, ld_out = X->ld), else it may not overlap it.
+ * Errors: INVALID_ARG, UNSUPPORTED (CSR), HIP_ERROR. */
+int wpsgd_dropout(const wpsgd_matrix *X, const int64_t *rows, int64_t n, double p, uint64_t seed, int chain, int64_t step, const int64_t *more_steps,
+                  void *out, int64_t ld_out, void *stream);
+
+/* A matrix in four bits, a scale for each group of 32, 64 or 128 elements of a row:
+ *   value(i, c) = v * scales[i*ld_scales + c/group],  v the code's value: 0, 1/2, 1, 3/2, 2, 3, 4, 6 for 0 .. 7 and their negatives for 8 .. 15
+ * Rows hold whole blocks of 128 elements in 64 bytes; element 32*j + 8*k + e (j, k < 4, e < 8) of a block is in its byte 16*k + 4*j + e/2, an even e in the lower half.
+ * Codes and scales behind the last column, as far as whole blocks go, are 0 (a product reads them). */
+typedef struct wpsgd_nibbles {
+    int64_t rows, cols;        /* rows < 2^31, 0 <= cols <= 2^31                                                        */
+    int group;                 /* 32, 64 or 128                                                                         */
+    void *codes;               /* DEVICE, 16-byte aligned                                                               */
+    int64_t ld;                /* row stride in bytes, a multiple of 16, >= 64*ceil(cols/128)                           */
+    void *scales;              /* DEVICE, bfloat16, 16-byte aligned                                                     */
+    int64_t ld_scales;         /* row stride in elements, a multiple of 8, >= 128/group * ceil(cols/128)                */
+} wpsgd_nibbles;
+
+/* Rows of the data set X (dense; CSR: UNSUPPORTED) in that form.  A group whose largest size is s has the least scale of 2^-126 or more that, times six, reaches s (1 for a group of zeros),
+ * and a code is the nearest value of x / scale, half to the even code.  A group with an element that is not finite has the scale NaN.
+ *   rows   as for wpsgd_quantize       out   its rows (= n), cols (= d) and group say so; codes and scales are written, as far as whole blocks go
+ * Errors: INVALID_ARG, UNSUPPORTED (CSR), HIP_ERROR. */
+int wpsgd_quantize_nibbles(const wpsgd_matrix *X, const int64_t *rows, int64_t n, const wpsgd_nibbles *out, void *stream);
+
+/* out[i*ld_out + j] = sum_c x(i, c) * W(j, c) for n rows of X (dense; CSR: UNSUPPORTED) and all rows j of W, made for few rows: every 64 of them read W once.  The values
+ * of x are taken as they are (fp32 ones too), sums are fp32, rounded once to dtype; parts of fp32 elements under 2^-126 may be lost.
+ *   rows   as for wpsgd_quantize       out   DEVICE, n x W->rows; it may not overlap X or W
+ * The result does not depend on timing.  Errors: INVALID_ARG, UNSUPPORTED (CSR), HIP_ERROR. */
+int wpsgd_nibble_matmul(const wpsgd_matrix *X, const int64_t *rows, int64_t n, const wpsgd_nibbles *W, void *out, int64_t ld_out, wpsgd_dtype dtype,
+                  void *stream);
+
 /* ---- diagnostics ---- */
 /* Streaming ceiling probe (not a step of the method): `groups` workgroups of 256 threads each read
  * `rows_per_group` rows of the dense matrix X, in the order the sample stream of chain = group index

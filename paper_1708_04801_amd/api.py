@@ -34,7 +34,8 @@ EXPORTS = [
     "wpsgd_quantize", "wpsgd_block_matmul_workspace", "wpsgd_block_matmul",
     "wpsgd_softmax_loss", "wpsgd_tensor_list_bytes", "wpsgd_tensor_list_make",
     "wpsgd_grad_norm_workspace", "wpsgd_grad_norm", "wpsgd_clip_grads", "wpsgd_clipped_step",
-    "wpsgd_draw_classes",
+    "wpsgd_draw_classes", "wpsgd_policy_loss", "wpsgd_preference_loss_workspace", "wpsgd_preference_loss",
+    "wpsgd_dropout", "wpsgd_quantize_nibbles", "wpsgd_nibble_matmul",
 ]
 
 
@@ -54,6 +55,11 @@ class _CPlan(ctypes.Structure):
 class _CBlocks(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("codes", ctypes.c_void_p), ("ld", ctypes.c_int64),
                 ("exps", ctypes.c_void_p), ("ld_exps", ctypes.c_int64)]
+
+
+class _CNibbles(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("group", ctypes.c_int), ("codes", ctypes.c_void_p), ("ld", ctypes.c_int64),
+                ("scales", ctypes.c_void_p), ("ld_scales", ctypes.c_int64)]
 
 
 class _CTensor(ctypes.Structure):
@@ -139,6 +145,14 @@ def load():
     L.wpsgd_clip_grads.argtypes = [pl, f64, vp, vp, sz, vp]
     L.wpsgd_clipped_step.argtypes = [pl, f64, f64, f64, vp, vp, sz, vp]
     L.wpsgd_draw_classes.argtypes = [vp, i64, i64, i64, ci, vp, ctypes.POINTER(_CDrawRule), vp, vp, vp]
+    L.wpsgd_policy_loss.argtypes = [vp, i64, i64, i64, ci, vp, vp, vp, vp, vp, f64, f64, f64, f64, vp, vp, vp, i64, vp]
+    L.wpsgd_preference_loss_workspace.argtypes = [i64]
+    L.wpsgd_preference_loss_workspace.restype = sz
+    L.wpsgd_preference_loss.argtypes = [vp, i64, i64, i64, ci, vp, vp, i64, vp, vp, vp, ci, f64, f64, f64, vp, vp, vp, i64, vp, sz, vp]
+    L.wpsgd_dropout.argtypes = [pm, vp, i64, f64, u64, ci, i64, vp, vp, i64, vp]
+    pn = ctypes.POINTER(_CNibbles)
+    L.wpsgd_quantize_nibbles.argtypes = [pm, vp, i64, pn, vp]
+    L.wpsgd_nibble_matmul.argtypes = [pm, vp, i64, pn, vp, i64, ci, vp]
     _lib = L
     return L
 
@@ -772,3 +786,165 @@ def wpsgd_draw_classes(Z: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=
     if rc != OK:
         raise WpsgdError(rc, "wpsgd_draw_classes")
     return drawn, probs
+
+
+def _vector(t, like, n, dtype):
+    """The address of a contiguous vector of n on like's GPU; None stays None."""
+    if t is None:
+        return None
+    assert t.dtype == dtype and t.is_contiguous() and t.numel() == n
+    return t.data_ptr()
+
+
+def _gradient(grad, Z, n, c, stream):
+    """(tensor, address, row stride) of a gradient of the scores Z: True for a new one, a tensor to write, or False for none."""
+    if grad is True:
+        grad = _new(Z, (n, c), Z.dtype, stream)
+        return grad, grad.data_ptr(), c
+    if grad is False or grad is None:
+        return None, None, 0
+    gn, gc, ld = _rows_of(grad)
+    assert grad.dtype == Z.dtype and gn == n and gc == c and grad.get_device() == Z.get_device()
+    return grad, grad.data_ptr(), ld
+
+
+def wpsgd_policy_loss(Z: torch.Tensor, drawn: torch.Tensor, advantage: torch.Tensor, old_log: Optional[torch.Tensor] = None,
+                      ref_log: Optional[torch.Tensor] = None, row_weights: Optional[torch.Tensor] = None, clip_low=0.2, clip_high=0.2, kl=0.0, scale=1.0,
+                      loss: Optional[torch.Tensor] = None, log_prob: Optional[torch.Tensor] = None, grad=True, stream=None):
+    """(loss, log_prob, grad): the rows' clipped policy losses of the classes drawn (int64, negative: does not count), these classes' log probabilities (float32), and
+    the gradient of scale * sum(loss) with respect to the scores Z, in Z's type.  advantage, old_log (when the classes were drawn; None: these
+    scores' own), ref_log (under a reference; needed where kl > 0) and row_weights: float32, one for each row.
+    grad: True for a new tensor, a tensor to write (Z itself too), or False for none."""
+    n, c, ld = _rows_of(Z)
+    index = _beside(Z, drawn, advantage, old_log, ref_log, row_weights, loss, log_prob)
+    if loss is None:
+        loss = _new(Z, n, torch.float32, stream)
+    if log_prob is None:
+        log_prob = _new(Z, n, torch.float32, stream)
+    f32 = torch.float32
+    grad, g_ptr, g_ld = _gradient(grad, Z, n, c, stream)
+    rc = _call(load().wpsgd_policy_loss, index, stream, Z.data_ptr(), n, c, ld, _DTYPES[Z.dtype], _vector(drawn, Z, n, torch.int64), _vector(old_log, Z, n, f32),
+               _vector(ref_log, Z, n, f32), _vector(advantage, Z, n, f32), _vector(row_weights, Z, n, f32), clip_low, clip_high, kl, scale,
+               _vector(loss, Z, n, f32), _vector(log_prob, Z, n, f32), g_ptr, g_ld)
+    if rc != OK:
+        raise WpsgdError(rc, "wpsgd_policy_loss")
+    return loss, log_prob, grad
+
+
+def wpsgd_preference_loss_workspace(n) -> int:
+    return int(load().wpsgd_preference_loss_workspace(int(n)))
+
+
+def wpsgd_preference_loss(Z: torch.Tensor, labels: torch.Tensor, offsets: torch.Tensor, ref_log: Optional[torch.Tensor] = None,
+                          row_weights: Optional[torch.Tensor] = None, pair_weights: Optional[torch.Tensor] = None, kind=LOGISTIC, beta=0.1, smoothing=0.0, scale=1.0,
+                          loss: Optional[torch.Tensor] = None, margin: Optional[torch.Tensor] = None, grad=True, workspace: Optional[torch.Tensor] = None,
+                          stream=None):
+    """(loss, margin, grad): the pairs' losses and margins (float32) and the gradient of scale * sum(loss) with respect to the scores Z, in Z's type.  Rows
+    offsets[2p] .. offsets[2p+1]-1 of Z are pair p's preferred sequence, those up to offsets[2p+2]-1 the other; labels (int64) as for wpsgd_softmax_loss, ref_log and
+    row_weights one float32 for each row, pair_weights for each pair.  kind: HINGE or LOGISTIC.
+    grad: True for a new tensor, a tensor to write (Z itself too), or False for none."""
+    n, c, ld = _rows_of(Z)
+    index = _beside(Z, labels, offsets, ref_log, row_weights, pair_weights, loss, margin, workspace)
+    ends = offsets.numel()
+    assert ends % 2 == 1
+    pairs, f32 = ends // 2, torch.float32
+    if loss is None:
+        loss = _new(Z, pairs, f32, stream)
+    if margin is None:
+        margin = _new(Z, pairs, f32, stream)
+    grad, g_ptr, g_ld = _gradient(grad, Z, n, c, stream)
+    L = load()
+    p, size, held = _call_workspace(workspace, L.wpsgd_preference_loss_workspace(n), Z, stream)
+    rc = _call(L.wpsgd_preference_loss, index, stream, Z.data_ptr(), n, c, ld, _DTYPES[Z.dtype], _vector(labels, Z, n, torch.int64),
+               _vector(offsets, Z, ends, torch.int64), pairs, _vector(ref_log, Z, n, f32), _vector(row_weights, Z, n, f32), _vector(pair_weights, Z, pairs, f32), kind,
+               beta, smoothing, scale, _vector(loss, Z, pairs, f32), _vector(margin, Z, pairs, f32), g_ptr, g_ld, p, size)
+    if rc != OK:
+        raise WpsgdError(rc, "wpsgd_preference_loss")
+    return loss, margin, grad
+
+
+def _picked(X, rows, name):
+    """(the C struct, the tensor, n, the address of the row numbers) of the rows that a call takes of a dense data set."""
+    cm, source = X.c_struct(), X.dense
+    if source is None:
+        raise WpsgdError(UNSUPPORTED, name)
+    if rows is None:
+        return cm, source, X.m, None
+    assert rows.dtype == torch.int64 and rows.is_contiguous() and rows.get_device() == source.get_device()
+    return cm, source, rows.numel(), rows.data_ptr()
+
+
+def wpsgd_dropout(X: Matrix, p, seed, chain=0, step=0, rows: Optional[torch.Tensor] = None, more_steps: Optional[torch.Tensor] = None,
+                  out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Rows of a dense data set (all, or those that `rows`, int64 on the GPU, names), each element dropped with probability p or scaled by
+    1 / (1 - p), by the generator's numbers for (seed, chain, step + more_steps, row of the result, column).  With the result's gradient as X, all rows, it is the gradient of the
+    rows.  more_steps: one int64 on the GPU, read when the work runs.  out: a tensor to write (X.dense too, where all rows are taken)."""
+    cm, source, n, picked = _picked(X, rows, "wpsgd_dropout")
+    index = _beside(source, more_steps, out)
+    if out is None:
+        out = _new(source, (n, X.d), source.dtype, stream)
+        ld = X.d
+    else:
+        assert out.dtype == source.dtype and out.shape == (n, X.d) and (out.numel() == 0 or out.stride(1) == 1)
+        ld = out.stride(0) if n > 1 else max(out.stride(0), X.d)
+    rc = _call(load().wpsgd_dropout, index, stream, ctypes.byref(cm), picked, n, p, seed, chain, step, _vector(more_steps, source, 1, torch.int64), out.data_ptr(), ld)
+    if rc != OK:
+        raise WpsgdError(rc, "wpsgd_dropout")
+    return out
+
+
+@dataclass
+class NibbleMatrix:
+    """rows x cols in four bits, a bfloat16 scale for each group of 32, 64 or 128 elements of a row: codes uint8 [rows, 64 for each block of 128 columns], scales bfloat16
+    [rows, groups, padded to whole eights].  wpsgd_quantize_nibbles makes one; the order of the codes in a block is include/wpsgd.h's."""
+    rows: int
+    cols: int
+    group: int
+    codes: torch.Tensor
+    scales: torch.Tensor
+
+    def c_struct(self) -> _CNibbles:
+        codes, scales, rows, blocks = self.codes, self.scales, self.rows, (self.cols + 127) // 128
+        assert codes.is_cuda and scales.is_cuda and codes.dtype == torch.uint8 and scales.dtype == torch.bfloat16 and self.group in (32, 64, 128)
+        (r0, c0), (r1, c1), (ld, step), (ld_scales, step_scales) = codes.shape, scales.shape, codes.stride(), scales.stride()
+        assert r0 == r1 == rows and c0 >= 64 * blocks and c1 >= 128 // self.group * blocks
+        assert step == step_scales == 1 or rows == 0 or blocks == 0
+        if rows == 1:
+            ld, ld_scales = 64 * blocks, -(-128 // self.group * blocks // 8) * 8
+        return _CNibbles(rows, self.cols, self.group, codes.data_ptr(), ld, scales.data_ptr(), ld_scales)
+
+
+def wpsgd_quantize_nibbles(X: Matrix, group=128, rows: Optional[torch.Tensor] = None, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+                    stream=None) -> NibbleMatrix:
+    """Rows of a dense data set (all, or those that `rows`, int64 on the GPU, names) as a NibbleMatrix with a scale for each `group` columns: 32, 64 or 128."""
+    cm, source, n, picked = _picked(X, rows, "wpsgd_quantize_nibbles")
+    index = _beside(source, codes, scales)
+    assert group in (32, 64, 128)
+    blocks = -(-X.d // 128)
+    if codes is None:
+        codes = _new(source, (n, 64 * blocks), torch.uint8, stream)
+    if scales is None:
+        scales = _new(source, (n, -(-(128 // group * blocks) // 8) * 8), torch.bfloat16, stream)
+    out = NibbleMatrix(n, X.d, group, codes, scales)
+    rc = _call(load().wpsgd_quantize_nibbles, index, stream, ctypes.byref(cm), picked, n, ctypes.byref(out.c_struct()))
+    if rc != OK:
+        raise WpsgdError(rc, "wpsgd_quantize_nibbles")
+    return out
+
+
+def wpsgd_nibble_matmul(X: Matrix, W: NibbleMatrix, rows: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, dtype=torch.bfloat16,
+                  stream=None) -> torch.Tensor:
+    """out[i, j] = sum_c x[i, c] W[j, c], float32 or bfloat16, for rows x of a dense data set (all, or those that `rows`, int64 on the GPU, names): few rows against many."""
+    cm, source, n, picked = _picked(X, rows, "wpsgd_nibble_matmul")
+    index = _beside(source, W.codes, W.scales, out)
+    if out is None:
+        assert dtype in _DTYPES
+        out = _new(source, (n, W.rows), dtype, stream)
+        ld = W.rows
+    else:
+        assert out.dtype in _DTYPES and out.shape == (n, W.rows) and (out.numel() == 0 or out.stride(1) == 1)
+        ld = out.stride(0) if n > 1 else max(out.stride(0), W.rows)
+    rc = _call(load().wpsgd_nibble_matmul, index, stream, ctypes.byref(cm), picked, n, ctypes.byref(W.c_struct()), out.data_ptr(), ld, _DTYPES[out.dtype])
+    if rc != OK:
+        raise WpsgdError(rc, "wpsgd_nibble_matmul")
+    return out

@@ -42,6 +42,10 @@ UNITS = [
     ("block_quantize", "block_quantize.hip", []),
     ("block_matmul", "block_matmul.hip", []),
     ("softmax_loss", "softmax_loss.hip", []),
+    ("policy_loss", "policy_loss.hip", []),
+    ("preference_loss", "preference_loss.hip", []),
+    ("dropout", "dropout.hip", []),
+    ("four_bits", "four_bits.hip", []),
     ("tensor_step", "tensor_step.hip", []),
     ("draw_classes", "draw_classes.hip", []),
     ("chain_csr_pair", "chain_csr_pair.hip", []),

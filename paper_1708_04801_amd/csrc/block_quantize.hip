@@ -42,21 +42,6 @@ struct QuantizeArgs {
     int64_t first;             // workgroup of the call at which the launch begins
 };
 
-template <typename T>
-__device__ inline void load8(const T *p, int64_t left, float (&x)[8])
-{
-    if (left >= 8) {
-        Bytes16 q[8 / Elem<T>::kPer16];
-#pragma unroll
-        for (int i = 0; i < 8 / Elem<T>::kPer16; ++i) q[i] = load16(p + i * Elem<T>::kPer16);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = Elem<T>::get(q[j / Elem<T>::kPer16].w, j % Elem<T>::kPer16);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = j < left ? Elem<T>::load(p + j) : 0.0f;
-    }
-}
-
 // Sixteen lanes to a block of 128, eight elements to a lane.
 template <typename T>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantizeArgs a)

@@ -45,6 +45,22 @@ __device__ inline uint32_t bf16_pack(float a, float b)
 }
 __device__ inline void Elem<uint16_t>::put(uint16_t *p, float v) { *(global_ptr<uint16_t>)p = (uint16_t)bf16_pack(v, v); }
 
+// eight elements, of which the first `left` are there; 0 for the others
+template <typename T>
+__device__ inline void load8(const T *p, int64_t left, float (&x)[8])
+{
+    if (left >= 8) {
+        Bytes16 q[8 / Elem<T>::kPer16];
+#pragma unroll
+        for (int i = 0; i < 8 / Elem<T>::kPer16; ++i) q[i] = load16(p + i * Elem<T>::kPer16);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = Elem<T>::get(q[j / Elem<T>::kPer16].w, j % Elem<T>::kPer16);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = j < left ? Elem<T>::load(p + j) : 0.0f;
+    }
+}
+
 __device__ inline float wave_max(float v)
 {
     // (fmaxf drops a NaN; the callers that want it kept look for it in the sums)

@@ -1,0 +1,199 @@
+// Loss of paired log ratios, with its gradient.  With l_i the log probability of row i's class and g_i = r_i (l_i - ref_i), a pair p of sequences of rows, the first of them
+// preferred, has the margin
+//   h_p = beta (sum of g_i over its first sequence - sum of g_i over its second),
+//   loss_p = w_p ((1 - eps) L(h_p) + eps L(-h_p)),   L(h) = max(0, 1 - h) or log(1 + exp(-h)),
+//   grad_ic = f_i (softmax(z_i)_c - [c = label_i]),  f_i = -+ scale beta r_i w_p ((1 - eps) L'(h_p) - eps L'(-h_p)).
+// A row's gradient waits for its whole pair, so the scores are read twice: row_softmax.h's pass leaves each row's statistics and g_i, a wave a pair adds those up (in fp64,
+// in an order that depends on the lengths alone) and leaves each row's f_i, and the last pass forms the gradient.
+#include "row_softmax.h"
+
+namespace wpsgd {
+
+struct RowResult {             // of the first pass, in the workspace
+    float2 *state;             // m_i and s_i
+    float *factor;             // 0, and f_i from the second pass on
+    double *gain;              // g_i
+};
+
+struct GainOfRow {
+    static constexpr bool kOneWave = true;
+    RowResult to;
+    const float *ref_log;
+    const int64_t *ends;       // where the first sequence begins
+    int64_t sequences;
+    // (what no sequence holds is not looked at)
+    __device__ bool counts(int64_t row, int64_t label, float r) const { return !(label < 0 || r == 0.0f) && row >= ends[0] && row < ends[sequences]; }
+    __device__ void absent(int64_t row) const
+    {
+        to.factor[row] = 0.0f;
+        to.gain[row] = 0.0;
+    }
+    __device__ float make(int64_t row, float r, const RowState &x, bool writes) const
+    {
+        constexpr double kInf = __builtin_inf();
+        const double l = x.unknown ? __builtin_nan("") : x.empty ? -kInf : ((double)x.z_label - (double)x.m) - log((double)x.s);
+        const double ref = ref_log ? (double)ref_log[row] : 0.0;
+        if (writes) {
+            to.state[row] = make_float2(x.m, x.s);
+            to.factor[row] = 0.0f;
+            to.gain[row] = l == -kInf && ref == -kInf ? 0.0 : (double)r * (l - ref);
+        }
+        return 0.0f;
+    }
+};
+
+struct PairArgs {
+    const int64_t *labels, *offsets;
+    int64_t n, pairs;
+    const float *row_weights, *pair_weights;
+    int hinge;
+    double beta, smoothing, scale;
+    RowResult rows;
+    float *loss, *margin;
+    int64_t first;
+};
+
+// L(h) and L'(h)
+__device__ inline double pair_loss(double h, bool hinge, double &slope)
+{
+    if (hinge) {
+        slope = h < 1.0 ? -1.0 : h == h ? 0.0 : h;
+        return h < 1.0 ? 1.0 - h : h == h ? 0.0 : h;
+    }
+    const double e = exp(-fabs(h));
+    slope = -(h >= 0.0 ? e : 1.0) / (1.0 + e);
+    return (h < 0.0 ? -h : 0.0) + log1p(e);
+}
+
+__global__ __launch_bounds__(256) void pair_kernel(PairArgs a)
+{
+    const int64_t p = (a.first + blockIdx.x) * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    if (p >= a.pairs) return;
+    const int64_t from = a.offsets[2 * p], middle = a.offsets[2 * p + 1], to = a.offsets[2 * p + 2];
+    if (from < 0 || middle < from || to < middle || to > a.n) {                   // no such rows
+        if (lane == 0) a.loss[p] = a.margin[p] = __builtin_nanf("");
+        return;
+    }
+    double sum = 0.0;
+    for (int64_t i = from + lane; i < to; i += 64) sum += i < middle ? a.rows.gain[i] : -a.rows.gain[i];
+    sum = wave_sum(sum);
+    const double h = a.beta * sum, w = a.pair_weights ? (double)a.pair_weights[p] : 1.0;
+    double slope, back;
+    double loss = pair_loss(h, a.hinge != 0, slope);
+    if (a.smoothing != 0.0) {
+        loss = (1.0 - a.smoothing) * loss + a.smoothing * pair_loss(-h, a.hinge != 0, back);
+        slope = (1.0 - a.smoothing) * slope - a.smoothing * back;
+    }
+    if (lane == 0) {
+        a.loss[p] = w == 0.0 ? 0.0f : (float)(w * loss);
+        a.margin[p] = (float)h;
+    }
+    if (w == 0.0) return;
+    const double f = -a.scale * a.beta * w * slope;
+    for (int64_t i = from + lane; i < to; i += 64) {
+        const double r = a.row_weights ? (double)a.row_weights[i] : 1.0;
+        if (a.labels[i] >= 0 && r != 0.0) a.rows.factor[i] = (float)(i < middle ? f * r : -f * r);
+    }
+}
+
+// The gradient, one row to NT threads, from the last row on: what the first pass read last may still be in the caches.
+template <typename T, int NT>
+__global__ __launch_bounds__(256) void pair_gradient_kernel(RowArgs a, RowResult rows)
+{
+    constexpr int E = Elem<T>::kPer16, kRows = 256 / NT;
+    const int64_t place = (a.first + blockIdx.x) * kRows + threadIdx.x / NT;
+    if (place >= a.n) return;
+    const int64_t row = a.n - 1 - place;
+    const int t = threadIdx.x % NT;
+    const T *z = static_cast<const T *>(a.z) + row * a.ld;
+    T *g = static_cast<T *>(a.grad) + row * a.ld_grad;
+    const int c = (int)a.c, vectors = c / E, tail = c - vectors * E;
+    const float f = rows.factor[row];
+    const float2 x = f != 0.0f ? rows.state[row] : make_float2(0.0f, 0.0f);
+    if (f == 0.0f || x.y == 0.0f) {                                               // does not count, or has no class left
+        for (int v = t; v < vectors; v += NT) store16(g + (int64_t)v * E, Bytes16{{0, 0, 0, 0}});
+        if (t < tail) Elem<T>::put(g + (int64_t)vectors * E + t, 0.0f);
+        return;
+    }
+    const int64_t label = a.labels[row];
+    const int at_label = label < a.c ? (int)label : -1;
+    const float base = x.x, over = f / x.y;
+    for (int v = t; v < vectors; v += NT) {
+        const Bytes16 q = load16(z + (int64_t)v * E);
+        float p[E];
+#pragma unroll
+        for (int j = 0; j < E; ++j) p[j] = exp_of<T>(Elem<T>::get(q.w, j) - base) * over;
+        if (at_label / E == v && at_label >= 0) {
+#pragma unroll
+            for (int j = 0; j < E; ++j) p[j] = at_label % E == j ? p[j] - f : p[j];
+        }
+        Bytes16 o;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (E == 8) o.w[j] = bf16_pack(p[2 * j], p[2 * j + 1]);
+            else o.w[j] = __float_as_uint(p[j]);
+        }
+        store16(g + (int64_t)v * E, o);
+    }
+    if (t < tail) {
+        const int at = vectors * E + t;
+        const float p = exp_of<T>(Elem<T>::load(z + at) - base) * over;
+        Elem<T>::put(g + at, at_label == at ? p - f : p);
+    }
+}
+
+template <typename T>
+static hipError_t launch_preference(RowArgs a, const GainOfRow &op, PairArgs p, void *grad, hipStream_t s)
+{
+    hipError_t e = launch_rows_softmax<T>(a, op, s);
+    if (e == hipSuccess)
+        e = in_launches((p.pairs + 3) / 4, 256, [&](int64_t first, unsigned count) {
+            p.first = first;
+            hipLaunchKernelGGL(pair_kernel, dim3(count), dim3(256), 0, s, p);
+        });
+    if (e != hipSuccess || !grad) return e;
+    a.grad = grad;
+    const bool small = a.c <= 64 * 4 * Elem<T>::kPer16;
+    return in_launches(small ? (a.n + 3) / 4 : a.n, 256, [&](int64_t first, unsigned count) {
+        a.first = first;
+        if (small) hipLaunchKernelGGL((pair_gradient_kernel<T, 64>), dim3(count), dim3(256), 0, s, a, op.to);
+        else hipLaunchKernelGGL((pair_gradient_kernel<T, 256>), dim3(count), dim3(256), 0, s, a, op.to);
+    });
+}
+
+}  // namespace wpsgd
+
+using namespace wpsgd;
+
+extern "C" {
+
+size_t wpsgd_preference_loss_workspace(int64_t n)
+{
+    if (n <= 0 || n > 0x7FFFFFFFLL) return 0;
+    return ((size_t)n * 20 + 255) / 256 * 256;
+}
+
+int wpsgd_preference_loss(const void *Z, int64_t n, int64_t classes, int64_t ld, wpsgd_dtype dtype, const int64_t *labels, const int64_t *offsets, int64_t pairs,
+                          const float *ref_log, const float *row_weights, const float *pair_weights, wpsgd_loss kind, double beta, double smoothing, double scale,
+                          float *loss, float *margin, void *grad, int64_t ld_grad, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if ((kind != WPSGD_HINGE && kind != WPSGD_LOGISTIC) || pairs < 0 || pairs > 0x3FFFFFFFLL) return WPSGD_INVALID_ARG;
+    if (!(beta - beta == 0.0) || !(scale - scale == 0.0) || !(smoothing >= 0.0 && smoothing <= 1.0)) return WPSGD_INVALID_ARG;
+    const int rc = check_scores(Z, n, classes, ld, dtype, grad, ld_grad);
+    if (rc != WPSGD_OK) return rc;
+    if (!offsets || (n > 0 && !labels) || (pairs > 0 && (!loss || !margin))) return WPSGD_INVALID_ARG;
+    const size_t need = wpsgd_preference_loss_workspace(n);
+    if (need && (!workspace || (uintptr_t)workspace % 256 != 0)) return WPSGD_INVALID_ARG;
+    if (workspace_bytes < need) return WPSGD_WORKSPACE_TOO_SMALL;
+    const RowResult to{reinterpret_cast<float2 *>(static_cast<double *>(workspace) + n), reinterpret_cast<float *>(static_cast<double *>(workspace) + 2 * n),
+                       static_cast<double *>(workspace)};
+    const RowArgs a{Z, n, classes, ld, labels, row_weights, nullptr, ld_grad, 0};
+    const GainOfRow op{to, ref_log, offsets, 2 * pairs};
+    const PairArgs p{labels, offsets, n, pairs, row_weights, pair_weights, kind == WPSGD_HINGE, beta, smoothing, scale, to, loss, margin, 0};
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const hipError_t e = dtype == WPSGD_F32 ? launch_preference<float>(a, op, p, grad, s) : launch_preference<uint16_t>(a, op, p, grad, s);
+    return e == hipSuccess ? WPSGD_OK : hip_fail(e);
+}
+
+}  // extern "C"

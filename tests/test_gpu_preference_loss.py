@@ -1,0 +1,213 @@
+"""The loss of paired log ratios and its gradient, against the formula in 64 bits and against differences."""
+import math
+
+import pytest
+import torch
+
+import answer_reference as ref
+from paper_1708_04801_amd import api
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+DELTA = 3e-4            # of a probability, and as much of a log of a row's sum: as for the softmax loss
+
+
+class Case:
+    def __init__(self, ends, c, dtype, seed, behind=0, pad=0, hinge=False, beta=0.3, eps=0.0, scale=0.5, weighted=True, spread=3.0):
+        g = torch.Generator().manual_seed(seed)
+        n = ends[-1] + behind
+        self.ends, self.hinge, self.beta, self.eps, self.scale, self.n = ends, hinge, beta, eps, scale, n
+        self.z = (torch.randn(n, c + pad, generator=g) * spread).to(DTYPES[dtype]).cuda()[:, :c]
+        self.labels = torch.randint(0, c, (n,), generator=g)
+        l = torch.log_softmax(self.z.double().cpu(), 1)[torch.arange(n), self.labels] if n else torch.zeros(0)
+        self.ref = (l + 0.7 * torch.randn(n, generator=g)).float()
+        self.w = torch.rand(n, generator=g) + 0.5 if weighted else torch.ones(n)
+        pairs = len(ends) // 2
+        self.pw = torch.rand(pairs, generator=g) + 0.5 if weighted else torch.ones(pairs)
+        self.weighted = weighted
+
+    def run(self, z=None, **more):
+        kind = api.HINGE if self.hinge else api.LOGISTIC
+        return api.wpsgd_preference_loss(self.z if z is None else z, self.labels.cuda(), torch.tensor(self.ends).cuda(), ref_log=self.ref.cuda(),
+                                         row_weights=self.w.float().cuda() if self.weighted else None, pair_weights=self.pw.float().cuda() if self.weighted else None,
+                                         kind=kind, beta=self.beta, smoothing=self.eps, scale=self.scale, **more)
+
+    def want(self, z=None):
+        z = (self.z if z is None else z).double().cpu()
+        return ref.preference_loss(z, self.labels, self.ends, self.ref.tolist(), self.w.float(), self.pw.float(), self.hinge, self.beta, self.eps, self.scale)
+
+    def reach(self):
+        """how far a pair's margin may be off: its rows' log probabilities by DELTA each, one rounding"""
+        margin = self.want()[1]
+        off = [abs(self.beta) * DELTA * float(self.w[a:b].sum()) for a, b in zip(self.ends[:-2:2], self.ends[2::2])]
+        return margin, torch.tensor(off, dtype=torch.float64)
+
+    def check(self, got):
+        loss, margin, grad = (t.double().cpu() if t is not None else None for t in got)
+        want_loss, want_margin, want_grad, slopes = self.want()
+        _, off = self.reach()
+        fine = torch.isfinite(want_margin)
+        if self.hinge:                                # no margin within reach of a kink, where the slope is one or the other
+            assert ((want_margin.abs() - 1).abs() > 2 * off + 1e-5)[fine].all()
+        assert torch.equal(torch.isnan(want_margin), torch.isnan(margin)) and torch.equal(want_margin[~fine & ~torch.isnan(margin)], margin[~fine & ~torch.isnan(margin)])
+        assert ((margin - want_margin).abs() <= off + 2.0 ** -23 * want_margin.abs())[fine].all()
+        pw = self.pw.double()
+        assert torch.equal(torch.isnan(want_loss), torch.isnan(loss))
+        fine = torch.isfinite(want_loss)
+        assert ((loss - want_loss).abs() <= pw * off + 2.0 ** -23 * want_loss.abs() + 1e-37)[fine].all() and torch.equal(loss[~fine & ~torch.isnan(loss)], want_loss[~fine & ~torch.isnan(loss)])
+        if grad is None:
+            return
+        nan = torch.isnan(want_grad)
+        assert torch.equal(nan, torch.isnan(grad))
+        # a factor is the slope, which moves by at most a quarter of its margin, times scale, beta and the weights; each probability is off by DELTA of itself
+        bound = DELTA * want_grad.abs() + (2.0 ** -8 * want_grad.abs() if self.z.dtype == torch.bfloat16 else 0) + 1e-37
+        share = torch.softmax(self.z.double().cpu(), 1).nan_to_num(0.0)
+        share[torch.arange(self.n), self.labels.clamp(0, self.z.shape[1] - 1)] += 1
+        for p in range(len(pw)):
+            a, b = self.ends[2 * p], self.ends[2 * p + 2]
+            size = abs(self.scale * self.beta) * pw[p] * self.w[a:b].double()
+            moved = 0.0 if self.hinge else float(off[p]) / 4 if math.isfinite(off[p]) else 0.0
+            bound[a:b] += (size * (moved + 2.0 ** -22 * (1 + abs(float(slopes[p])) if not math.isnan(slopes[p]) else 1)))[:, None] * share[a:b]
+        assert ((grad - want_grad).abs() <= bound)[~nan].all()
+
+
+def ends_of(*lengths):
+    out = [0]
+    for v in lengths:
+        out.append(out[-1] + v)
+    return out
+
+
+SHAPES = [(ends_of(1, 1), 1, 0), (ends_of(1, 1), 2, 0), (ends_of(2, 1, 0, 3), 7, 1), (ends_of(0, 0, 4, 0), 65, 0), (ends_of(5, 9, 3, 4, 1, 1), 257, 3), (ends_of(3, 2, 4, 1), 1001, 0),
+          (ends_of(70, 130), 300, 0), (ends_of(2, 3, 1, 2), 4099, 8), (ends_of(4, 3), 20000, 1), (ends_of(1, 2, 2, 1), 65536, 0), (ends_of(1, 1), 131075, 0)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hinge", [False, True])
+@pytest.mark.parametrize("ends,c,pad", SHAPES)
+def test_loss_and_gradient_match_the_formula(ends, c, pad, hinge, dtype):
+    k = Case(ends, c, dtype, c + len(ends), behind=2, pad=pad, hinge=hinge)
+    keep = k.z.clone()
+    got = k.run()
+    k.check(got)
+    assert torch.equal(k.z, keep) and not got[2][ends[-1]:].any()
+    alone = k.run(grad=False)
+    assert alone[2] is None and torch.equal(alone[0], got[0]) and torch.equal(alone[1], got[1])
+    inside = k.run(grad=k.z)
+    assert torch.equal(inside[0], got[0]) and torch.equal(k.z, got[2])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hinge", [False, True])
+def test_settings(hinge, dtype):
+    for eps, beta, scale in ((0.0, 0.1, 1.0), (0.2, 0.4, -2.0), (1.0, -0.2, 0.3), (0.0, 0.0, 1.0)):
+        k = Case(ends_of(6, 4, 1, 5, 3, 3), 500, dtype, 17, hinge=hinge, eps=eps, beta=beta, scale=scale, weighted=False)
+        k.check(k.run())
+    k = Case(ends_of(2, 3, 1, 1), 90, dtype, 18, hinge=hinge, weighted=False, beta=0.03)
+    k.ref[:] = 0.0                                    # no reference
+    got = api.wpsgd_preference_loss(k.z, k.labels.cuda(), torch.tensor(k.ends).cuda(), kind=api.HINGE if hinge else api.LOGISTIC, beta=k.beta, scale=k.scale)
+    k.check(got)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("c", [6, 70, 1030, 9000, 140000])
+def test_masks_and_rows_that_do_not_count(c, dtype):
+    k = Case(ends_of(2, 2, 2, 2, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 2, 1), c, dtype, c, behind=3)
+    z, labels = k.z, k.labels
+    lowest = torch.finfo(DTYPES[dtype]).min
+    labels[0] = -1
+    z[0, 0] = math.nan                                # does not count
+    k.w[2] = 0.0
+    z[2] = math.inf
+    z[3, : c // 2] = lowest
+    labels[3] = c - 1
+    z[4] = lowest                                     # uniform
+    k.ref[4] = -math.log(c)
+    z[8] = -math.inf                                  # nothing left in the preferred sequence
+    z[11, int(labels[11])] = -math.inf                # the other's label masked
+    z[12, c // 2] = math.nan                          # not a number
+    labels[15] = c                                    # no such class
+    k.pw[6] = 0.0                                     # a pair without weight, whatever it holds
+    z[17, 0] = math.nan
+    z[18, int(labels[18])] = -math.inf                # masked under both models
+    k.ref[18] = -math.inf
+    z[-2] = math.nan                                  # in no sequence
+    z[-1] = -math.inf
+    labels[-3] = c + 5
+    got = k.run()
+    k.check(got)
+    loss, margin, grad = got
+    assert margin[2] == -math.inf and loss[2] == math.inf and not grad[8].any() and margin[3] == math.inf and loss[3] == 0
+    assert torch.isnan(grad[12:16]).all() and torch.isnan(loss[4:6]).all() and loss[6] == 0 and not grad[16:18].any()
+    assert torch.isfinite(loss[7]) and not grad[[0, 2]].any() and not grad[-3:].any()
+
+
+def test_bad_offsets_show_and_stay_inside():
+    k = Case(ends_of(3, 3, 2, 2), 50, "f32", 3)
+    for bad, lost in (([0, 3, 11, 8, 10], [0, 1]), ([-1, 3, 6, 8, 10], [0]), ([0, 3, 2, 8, 10], [0]), ([0, 3, 6, 8, 1 << 40], [1]), ([5, 4, 3, 2, 1], [0, 1])):
+        offsets = torch.tensor(bad).cuda()
+        loss, margin, grad = api.wpsgd_preference_loss(k.z, k.labels.cuda(), offsets, ref_log=k.ref.cuda())
+        assert torch.isnan(loss).nonzero()[:, 0].tolist() == lost and torch.isnan(margin).nonzero()[:, 0].tolist() == lost
+
+
+def test_gradient_matches_differences_of_the_loss():
+    h = 2.0 ** -5
+    k = Case(ends_of(2, 1, 1, 3), 30, "f32", 8, spread=1.5, beta=0.3, eps=0.1, scale=0.7)
+    grad = k.run()[2].double().cpu()
+    for i in range(k.n):
+        for j in range(30):
+            up, down = k.z.clone(), k.z.clone()
+            up[i, j] += h
+            down[i, j] -= h
+            lu, ld = (k.run(t, grad=False)[0].double().cpu() for t in (up, down))
+            slope = k.scale * float((lu - ld).sum()) / (2 * h)
+            # the margin's derivatives along one score are at most b = beta r <= 0.45 times 1, 1/4, 1/8, the loss's along the margin 1, 1/4, 1/8: third ones together
+            # (b^3 + 3 b b + b) / 8 < 0.2 of the pair's weight <= 1.5; two losses off by 2^-19
+            assert abs(float(grad[i, j]) - slope) <= k.scale * 1.5 * (0.2 * h * h / 6 + 2.0 ** -19 / h)
+
+
+def test_strides_workspace_and_outputs_of_the_callers():
+    k = Case(ends_of(2, 3, 4, 1), 333, "bf16", 9, pad=7)
+    room = torch.full((10, 350), 3.0, dtype=torch.bfloat16, device="cuda")
+    loss, margin = torch.empty(2, device="cuda"), torch.empty(2, device="cuda")
+    ws = torch.full((api.wpsgd_preference_loss_workspace(10) + 256,), 0xFF, dtype=torch.uint8, device="cuda")
+    got = k.run(grad=room[:, 5:338], loss=loss, margin=margin, workspace=ws)
+    want = k.run()
+    assert got[0] is loss and got[1] is margin and all(torch.equal(a, b) for a, b in zip(got, want))
+    assert (room[:, :5] == 3).all() and (room[:, 338:] == 3).all() and (ws[-256:] == 0xFF).all()
+
+
+def test_rows_behind_the_32_bit_offset():
+    n, c = 40000, 65536
+    z = torch.zeros((n, c), dtype=torch.bfloat16, device="cuda")
+    k = Case(ends_of(2, 1), c, "bf16", 4, weighted=False)
+    z[-3:] = k.z
+    labels = torch.full((n,), 1, dtype=torch.int64, device="cuda")
+    labels[-3:] = k.labels.cuda()
+    far = torch.zeros(n, device="cuda")
+    far[-3:] = k.ref.cuda()
+    got = api.wpsgd_preference_loss(z, labels, torch.tensor([n - 3, n - 1, n]).cuda(), ref_log=far, beta=0.3, scale=0.5, grad=z)
+    want = k.run()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[2][-3:], want[2]) and not got[2][:100].any()
+
+
+def test_refusals():
+    k = Case(ends_of(2, 2), 10, "f32", 1)
+    o, y = torch.tensor(k.ends).cuda(), k.labels.cuda()
+    for bad in (dict(beta=math.inf), dict(smoothing=-0.1), dict(smoothing=1.1), dict(scale=math.nan), dict(kind=7)):
+        with pytest.raises(api.WpsgdError) as e:
+            api.wpsgd_preference_loss(k.z, y, o, **bad)
+        assert e.value.status == api.INVALID_ARG
+    with pytest.raises(api.WpsgdError) as e:
+        api.wpsgd_preference_loss(k.z, y, o, workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))
+    assert e.value.status == api.WORKSPACE_TOO_SMALL
+    for bad in (lambda: api.wpsgd_preference_loss(k.z, y, o[:2]), lambda: api.wpsgd_preference_loss(k.z, y, o.int()), lambda: api.wpsgd_preference_loss(k.z, y[:3], o),
+                lambda: api.wpsgd_preference_loss(k.z, y, o, ref_log=torch.zeros(3, device="cuda")), lambda: api.wpsgd_preference_loss(k.z, y, o.cpu()),
+                lambda: api.wpsgd_preference_loss(k.z, y, o, pair_weights=torch.ones(2, device="cuda"))):
+        with pytest.raises(AssertionError):
+            bad()
+    got = api.wpsgd_preference_loss(k.z[:0], y[:0], torch.zeros(3, dtype=torch.int64, device="cuda"))
+    assert abs(float(got[0][0]) - math.log(2)) < 1e-6 and got[1][0] == 0 and got[2].shape == (0, 10)
+    got = api.wpsgd_preference_loss(k.z, y, torch.zeros(1, dtype=torch.int64, device="cuda"))
+    assert got[0].numel() == 0 and not got[2].any()

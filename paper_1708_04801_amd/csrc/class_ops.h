@@ -45,7 +45,8 @@ __device__ inline uint32_t bf16_pack(float a, float b)
 }
 __device__ inline void Elem<uint16_t>::put(uint16_t *p, float v) { *(global_ptr<uint16_t>)p = (uint16_t)bf16_pack(v, v); }
 
-// eight elements, of which the first `left` are there; 0 for the others
+// Eight elements, of which the first `left` (1 or more) are there; 0 for the others.  (Those that are not there ask for the last that is: all loads on their way at once, where a branch
+// around each would wait for one after the other.)
 template <typename T>
 __device__ inline void load8(const T *p, int64_t left, float (&x)[8])
 {
@@ -57,7 +58,9 @@ __device__ inline void load8(const T *p, int64_t left, float (&x)[8])
         for (int j = 0; j < 8; ++j) x[j] = Elem<T>::get(q[j / Elem<T>::kPer16].w, j % Elem<T>::kPer16);
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = j < left ? Elem<T>::load(p + j) : 0.0f;
+        for (int j = 0; j < 8; ++j) x[j] = Elem<T>::load(p + (j < left ? j : left - 1));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = j < left ? x[j] : 0.0f;
     }
 }
 

@@ -88,6 +88,7 @@ __global__ __launch_bounds__(256) void quantize4_kernel(Quantize4Args a)
 typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8v __attribute__((ext_vector_type(8)));
 typedef float f32x4v __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
 
 // the eight values of a word's codes, as they are
 __device__ inline bf16x8v widen_codes(uint32_t w)
@@ -97,21 +98,73 @@ __device__ inline bf16x8v widen_codes(uint32_t w)
     return bf16x8v{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
 }
 
-// fp32 values as sums of three bfloat16 values, eight significant bits each; what is not finite stays in the first
-__device__ inline void split8(const float (&x)[8], bf16x8v (&part)[3])
+// Values as bfloat16 (PARTS 1: they are), or as sums of three bfloat16 values, eight significant bits each: what a value's upper half stands for, the same of the rest, and the rest of that.
+// What is not finite stays in the first.
+template <int PARTS>
+__device__ inline void split8(const float (&x)[8], bf16x8v *part)
 {
+    const auto halves = [](const float (&v)[8]) {
+        u32x4v w;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const uint32_t bits = __float_as_uint(x[j]);
-        const bool finite = fabsf(x[j]) < __builtin_inff();
-        const float hi = finite ? __uint_as_float(bits & 0xFFFF0000u) : x[j];
-        const float rest = finite ? x[j] - hi : 0.0f;
-        const float mid = __uint_as_float(__float_as_uint(rest) & 0xFFFF0000u);
-        part[0][j] = (__bf16)hi;
-        part[1][j] = (__bf16)mid;
-        part[2][j] = (__bf16)(rest - mid);
+        for (int j = 0; j < 4; ++j) w[j] = __builtin_amdgcn_perm(__float_as_uint(v[2 * j + 1]), __float_as_uint(v[2 * j]), 0x07060302);
+        return __builtin_bit_cast(bf16x8v, w);
+    };
+    part[0] = halves(x);
+    if constexpr (PARTS == 3) {
+        float rest[8], last[8], most = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            rest[j] = x[j] - __uint_as_float(__float_as_uint(x[j]) & 0xFFFF0000u);
+            last[j] = rest[j] - __uint_as_float(__float_as_uint(rest[j]) & 0xFFFF0000u);
+            most += fabsf(rest[j]);                                                     // NaN where one is not finite
+        }
+        if (most != most) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                last[j] = rest[j] == rest[j] ? last[j] : 0.0f;
+                rest[j] = rest[j] == rest[j] ? rest[j] : 0.0f;
+            }
+        }
+        part[1] = halves(rest);
+        part[2] = halves(last);
     }
 }
+
+// Eight elements of a row of d from column col (a multiple of eight) on, in two steps, so that many loads can be on their way without a branch between them: ask() reads what lies in
+// the row there or before, give() is the elements if the row holds all eight, else zeros.  What a row ends with, where d is no multiple of eight, is put in by itself.
+template <typename T> struct Eight {
+    static constexpr int E = Elem<T>::kPer16;
+    Bytes16 q[8 / E];
+    // eight that are there for certain, and their parts
+    __device__ void ask(const T *p)
+    {
+#pragma unroll
+        for (int i = 0; i < 8 / E; ++i) q[i] = load16(p + i * E);
+    }
+    __device__ void parts(bf16x8v *part) const
+    {
+        if constexpr (E == 8) {
+            part[0] = __builtin_bit_cast(bf16x8v, q[0]);
+        } else {
+            float x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = Elem<T>::get(q[j / E].w, j % E);
+            split8<3>(x, part);
+        }
+    }
+    __device__ void ask(const T *row, int64_t col, int64_t d)
+    {
+        const T *p = row + (col + 8 <= d ? col : d >= 8 ? d - 8 : 0);
+#pragma unroll
+        for (int i = 0; i < 8 / E; ++i) q[i] = d >= 8 ? load16(p + i * E) : Bytes16{{0, 0, 0, 0}};
+    }
+    __device__ void give(int64_t col, int64_t d, bool there, float (&x)[8]) const
+    {
+        const bool whole = there && col + 8 <= d;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = whole ? Elem<T>::get(q[j / E].w, j % E) : 0.0f;
+    }
+};
 
 struct Matmul4Args {
     const void *x;
@@ -121,173 +174,519 @@ struct Matmul4Args {
     const uint16_t *scales;
     int64_t ld_codes, ld_scales, classes;
     int blocks;
-    int half;                  // results are bfloat16
+    bool half, wide;           // results are bfloat16; the rows are fp32
     void *out;
     int64_t ld_out;
     int64_t first, first_row;  // workgroup and row at which the launch begins
 };
 
-// The classes' codes go from memory straight into the matrix instructions, sixteen classes to a wave; the few rows lie in LDS as fragments, up to 64 KiB of the sum at a time, fp32
-// ones as three parts.  Row i of a tile is row 4 (i mod 4) + i / 4 of the instruction, so that up to four rows need one result register of a lane, up to eight two (R).  kWaves4 waves
-// to a workgroup: `along` of them share the blocks of the sum in turn and add up through LDS in their order, the others take the next classes.  A group's products are
-// summed by themselves and times its scale added in fp32.
-constexpr int kWaves4 = 8;
-template <int MT, int R, int PARTS> constexpr int held_blocks4()
+// Every other call.  The classes' codes go from memory straight into the matrix instructions, two blocks (a line of 128 bytes) of NT sixteens of classes at a time to a wave.  Row i of a
+// tile of sixteen rows is row 4 (i mod 4) + i / 4 of the instruction, so that up to four rows need one result register of a lane, up to eight two (R).  A group's products are summed by
+// themselves and times its scale added in fp32.  Of WAVES waves in a workgroup `along` share the sum, pairs of blocks in turn, and add up through LDS in their order; the others take the next
+// classes.  HELD: the rows lie in LDS as fragments, up to WAVES * 8 KiB of the sum at a time, fp32 ones as three parts; else each wave asks for its own part of them.
+// 8 x 65536 x 4096 fp32 (LDS) 43 us, 3.2 TB/s of codes; 1 x 4096 x 4096 (each wave) 7.1, a launch and three trips to memory one behind the other (row number, row, sum);
+// 64 x 65536 x 4096 73, 470 TFLOP/s: fragments from LDS and codes widened for four tiles of rows at a time.
+template <int MT, int R, int PARTS, int WAVES> constexpr int held_blocks4()
 {
     int n = 64;
-    while (n > 1 && n * MT * R * PARTS > 64) n /= 2;
+    while (n > 2 && n * MT * R * PARTS > WAVES * 8) n /= 2;
     return n;
 }
 
-template <typename T, int MT, int R, int G>
-__global__ __launch_bounds__(64 * kWaves4) void matmul4_kernel(Matmul4Args g, int along)
+// pairs of blocks on their way while one is worked on
+template <int MT, int R, int NT, int PARTS, int WAVES> constexpr int ahead4()
 {
-    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, kHeld = held_blocks4<MT, R, PARTS>(), kLanes = 16 * R;
-    constexpr int kAhead = 4;
+    const int pairs = held_blocks4<MT, R, PARTS, WAVES>() / 2, most = NT == 1 ? 4 : 2;
+    return pairs < most ? pairs : most;
+}
+// a barrier for what lies in LDS: loads from memory stay on their way
+__device__ inline void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+template <typename T, int MT, int R, int NT, int G, int WAVES, bool HELD>
+__global__ __launch_bounds__(64 * WAVES) void matmul4_kernel(Matmul4Args g, int along)
+{
+    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, kHeld = held_blocks4<MT, R, PARTS, WAVES>(), kLanes = 16 * R, kThreads = 64 * WAVES;
+    constexpr int kAhead = ahead4<MT, R, NT, PARTS, WAVES>();
+    constexpr int kSums = MT * NT * R;
     __shared__ union {
-        bf16x8v held[kHeld * MT * 4 * PARTS][kLanes];
-        f32x4v sums[kWaves4][MT][64];
+        bf16x8v held[HELD ? kHeld * MT * 4 * PARTS : 1][kLanes];
+        float sums[WAVES][kSums][64];
     } lds;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rho = lane & 15, k = lane >> 4;
-    const int across = kWaves4 / along, mine = wave % along;
-    const int64_t c0 = ((g.first + blockIdx.x) * across + wave / along) * 16, h0 = g.first_row + (int64_t)blockIdx.y * (16 * MT);
-    const bool idle = c0 >= g.classes, active = (rho & 3) < R;
-    const int place = k * (4 * R) + (rho >> 2) * R + (rho & 3);
-    f32x4v acc[MT];
-#pragma unroll
-    for (int t = 0; t < MT; ++t) acc[t] = f32x4v{0.0f, 0.0f, 0.0f, 0.0f};
-    const int64_t cls = c0 + rho < g.classes ? c0 + rho : g.classes - 1;
-    const uint8_t *codes = g.codes + cls * g.ld_codes + k * 16;
-    const uint16_t *scales = g.scales + cls * g.ld_scales;
-    uint4 q[kAhead];
-    uint2 sc[kAhead];
-    auto fetch = [&](int step, int j) {
-        const int b = step * along + mine, at = b < g.blocks ? b : g.blocks - 1;
-        q[j] = *reinterpret_cast<const uint4 *>(codes + (int64_t)at * 64);
-        if constexpr (G == 1) sc[j].x = scales[at];
-        else if constexpr (G == 2) sc[j].x = *reinterpret_cast<const uint32_t *>(scales + (int64_t)at * 2);
-        else sc[j] = *reinterpret_cast<const uint2 *>(scales + (int64_t)at * 4);
-    };
-    // a thread's pieces of a filling: eight elements of one row each, the same row in every piece (MT 4: in every other one)
-    constexpr int kPieces = kHeld * MT * 4 * kLanes, kEach = (kPieces + 511) / 512, kRowsOf = MT == 4 ? 2 : 1;
-    const T *from[kRowsOf];
-#pragma unroll
-    for (int y = 0; y < kRowsOf; ++y) {
-        const int piece = threadIdx.x + 512 * y, i = (piece >> 4) % (4 * R), t = (piece >> 4) / (4 * R) % MT;
-        const int64_t h = h0 + t * 16 + i, row = h < g.n ? (g.rows ? g.rows[h] : h) : -1;
-        from[y] = row >= 0 && row < g.m ? static_cast<const T *>(g.x) + row * g.ld : nullptr;
-    }
-    const int per = kHeld / along, steps = (g.blocks + kHeld - 1) / kHeld * per;        // of a wave between two fillings; the same for every wave
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) fetch(j, j);
-    for (int step0 = 0; step0 < steps; step0 += kAhead) {
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            const int step = step0 + j;
-            if (step >= steps) break;
-            if (step % per == 0) {
-                const int b0 = step / per * kHeld;
-                if (step > 0) __syncthreads();
-#pragma unroll
-                for (int y = 0; y < kEach; ++y) {
-                    const int piece = threadIdx.x + 512 * y;
-                    if (kPieces % 512 != 0 && piece >= kPieces) break;
-                    const int pk = piece & 3, pj = piece >> 2 & 3, i = (piece >> 4) % (4 * R), u = (piece >> 4) / (4 * R), t = u % MT, in = u / MT;
-                    const int64_t col = (int64_t)(b0 + in) * kNibbleBlock + pj * 32 + pk * 8;
-                    const T *p = from[kRowsOf == 2 ? y & 1 : 0];
-                    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-                    if (p && col < g.d) load8(p + col, g.d - col, x);
-                    bf16x8v part[3];
-                    if constexpr (PARTS == 3) {
-                        split8(x, part);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) part[0][e] = (__bf16)x[e];
-                    }
-                    const int to = pk * (4 * R) + (i & 3) * R + (i >> 2);
-#pragma unroll
-                    for (int e = 0; e < PARTS; ++e) lds.held[((in * MT + t) * 4 + pj) * PARTS + e][to] = part[e];
-                }
-                __syncthreads();
-            }
-            const int b = step * along + mine;
-            if (b < g.blocks && !idle) {
-                const uint32_t w[4] = {q[j].x, q[j].y, q[j].z, q[j].w};
-                bf16x8v f[4];
-#pragma unroll
-                for (int y = 0; y < 4; ++y) f[y] = widen_codes(w[y]);
-                const float s[4] = {bf16_lo(sc[j].x), G > 1 ? bf16_hi(sc[j].x) : 0.0f, G > 2 ? bf16_lo(sc[j].y) : 0.0f, G > 2 ? bf16_hi(sc[j].y) : 0.0f};
-                const int at = b % kHeld;
-#pragma unroll
-                for (int t = 0; t < MT; ++t) {
-                    f32x4v sum = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-#pragma unroll
-                        for (int e = 0; e < PARTS; ++e) {
-                            bf16x8v h = {};
-                            if (R == 4 || active) h = lds.held[((at * MT + t) * 4 + y) * PARTS + e][place];
-                            sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h, f[y], sum, 0, 0, 0);
-                        }
-                        if ((y + 1) % (4 / G) == 0) {
-#pragma unroll
-                            for (int r = 0; r < R; ++r) acc[t][r] = fmaf(sum[r], s[y / (4 / G)], acc[t][r]);
-                            sum = f32x4v{0.0f, 0.0f, 0.0f, 0.0f};
-                        }
-                    }
-                }
-            }
-            fetch(step + kAhead, j);
-        }
-    }
-    if (along > 1) {
-        __syncthreads();
-#pragma unroll
-        for (int t = 0; t < MT; ++t) lds.sums[wave][t][lane] = acc[t];
-        __syncthreads();
-        if (mine != 0) return;
-#pragma unroll
-        for (int t = 0; t < MT; ++t)
-            for (int w = 1; w < along; ++w) acc[t] += lds.sums[wave + w][t][lane];
-    }
-    if (c0 + rho >= g.classes) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rho = lane & 15, k = lane >> 4;
+    const int across = WAVES / along, mine = wave % along;
+    const int64_t c0 = ((g.first + blockIdx.x) * across + wave / along) * (16 * NT), h0 = g.first_row + (int64_t)blockIdx.y * (16 * MT);
+    const bool active = (rho & 3) < R;
+    float acc[MT][NT][R];
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int64_t h = h0 + t * 16 + 4 * r + k;
-            if (h >= g.n) continue;
-            if (g.half) Elem<uint16_t>::put(static_cast<uint16_t *>(g.out) + h * g.ld_out + c0 + rho, acc[t][r]);
-            else Elem<float>::put(static_cast<float *>(g.out) + h * g.ld_out + c0 + rho, acc[t][r]);
+        for (int u = 0; u < NT; ++u)
+#pragma unroll
+            for (int r = 0; r < R; ++r) acc[t][u][r] = 0.0f;
+    const uint8_t *codes[NT];
+    const uint16_t *scales[NT];
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+        const int64_t cls = c0 + u * 16 + rho < g.classes ? c0 + u * 16 + rho : g.classes - 1;
+        codes[u] = g.codes + cls * g.ld_codes + k * 16;
+        scales[u] = g.scales + cls * g.ld_scales;
+    }
+    struct Pair {
+        uint4 q[NT][2];
+        uint32_t s[NT][G];                                                              // 2 G scales
+    };
+    auto fetch = [&](Pair &p, int pair) {
+        const int last = g.blocks - 1, b = 2 * pair < last ? 2 * pair : last & ~1, next = b < last ? b + 1 : b;
+#pragma unroll
+        for (int u = 0; u < NT; ++u) {
+            p.q[u][0] = *reinterpret_cast<const uint4 *>(codes[u] + (int64_t)b * 64);
+            p.q[u][1] = *reinterpret_cast<const uint4 *>(codes[u] + (int64_t)next * 64);
+            const uint16_t *s = scales[u] + (int64_t)b * G;
+            if constexpr (G == 1) {
+                p.s[u][0] = *reinterpret_cast<const uint32_t *>(s);
+            } else if constexpr (G == 2) {
+                const uint2 v = *reinterpret_cast<const uint2 *>(s);
+                p.s[u][0] = v.x, p.s[u][1] = v.y;
+            } else {
+                const uint4 v = *reinterpret_cast<const uint4 *>(s);
+                p.s[u][0] = v.x, p.s[u][1] = v.y, p.s[u][2] = v.z, p.s[u][3] = v.w;
+            }
         }
+    };
+    // block `half` of a pair, with get(t, y, parts) the parts of tile t's fragment of the y-th 32 columns
+    auto multiply = [&](const Pair &p, int half, auto get) {
+        bf16x8v f[NT][4];
+#pragma unroll
+        for (int u = 0; u < NT; ++u) {
+            const uint4 q = p.q[u][half];
+            f[u][0] = widen_codes(q.x), f[u][1] = widen_codes(q.y), f[u][2] = widen_codes(q.z), f[u][3] = widen_codes(q.w);
+        }
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            f32x4v sum[NT];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                if (y % (4 / G) == 0) {
+#pragma unroll
+                    for (int u = 0; u < NT; ++u) sum[u] = f32x4v{0.0f, 0.0f, 0.0f, 0.0f};
+                }
+                bf16x8v h[PARTS];
+                get(t, y, h);
+#pragma unroll
+                for (int e = 0; e < PARTS; ++e)
+#pragma unroll
+                    for (int u = 0; u < NT; ++u) sum[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(h[e], f[u][y], sum[u], 0, 0, 0);
+                if ((y + 1) % (4 / G) == 0) {
+#pragma unroll
+                    for (int u = 0; u < NT; ++u) {
+                        const int at = half * G + y / (4 / G);
+                        const float s = (at & 1) ? bf16_hi(p.s[u][at >> 1]) : bf16_lo(p.s[u][at >> 1]);
+#pragma unroll
+                        for (int r = 0; r < R; ++r) acc[t][u][r] = fmaf(sum[u][r], s, acc[t][u][r]);
+                    }
+                }
+            }
+        }
+    };
+    const int pairs = (g.blocks + 1) / 2;
+    if constexpr (HELD) {
+        // A thread's pieces of a filling: eight elements of one row each, the same row in every piece (or in every other one), and a wave's pieces of four rows that follow each other.
+        // Loads come back in the order they are asked for: the rows' go out behind the first pair of the classes', the other pairs behind them.
+        constexpr int kPieces = kHeld * MT * 4 * kLanes, kEach = (kPieces + kThreads - 1) / kThreads, kRowsOf = kThreads / 16 >= MT * 4 * R ? 1 : MT * 4 * R / (kThreads / 16);
+        Pair p[kAhead];
+        fetch(p[0], mine);
+        const T *from[kRowsOf];
+        bool there[kRowsOf];
+#pragma unroll
+        for (int y = 0; y < kRowsOf; ++y) {
+            const int four = __builtin_amdgcn_readfirstlane((threadIdx.x + kThreads * y) >> 6) * 4, i = four % (4 * R), t = four / (4 * R) % MT;
+            const int64_t h = h0 + t * 16 + i;
+            int64_t row = -1;
+#pragma unroll
+            for (int o = 0; o < 4; ++o) {                                               // (by scalar loads, which wait for themselves)
+                const int64_t one = h + o < g.n ? (g.rows ? g.rows[h + o] : h + o) : -1;
+                row = (lane >> 4) == o ? one : row;
+            }
+            there[y] = row >= 0 && row < g.m;
+            from[y] = static_cast<const T *>(g.x) + (there[y] ? row * g.ld : 0);
+        }
+        const int place = k * (4 * R) + (rho >> 2) * R + (rho & 3);
+        const int per = kHeld / 2 / along, steps = (pairs + along - 1) / along;            // of a wave between two fillings, and in all: the same for every wave
+        // a filling from block b0 on: between(), once the loads are on their way; whole: it ends within the rows
+        auto fill = [&](int b0, auto between) {
+            Eight<T> got[kEach];
+            constexpr int kNext = kThreads / (16 * 4 * R * MT) * kNibbleBlock;           // columns from a piece to the thread's next one (of the same row)
+            const int v0 = (threadIdx.x >> 4) / (4 * R) / MT, in_block = (threadIdx.x >> 2 & 3) * 32 + (threadIdx.x & 3) * 8;
+            const int64_t col0 = (int64_t)(b0 + v0) * kNibbleBlock + in_block;
+            const bool whole = kRowsOf == 1 && kPieces % kThreads == 0 && (int64_t)(b0 + kHeld) * kNibbleBlock <= g.d;
+            auto col_of = [&](int y) { return kRowsOf == 1 ? col0 + y * kNext : (int64_t)(b0 + ((threadIdx.x + kThreads * y) >> 4) / (4 * R) / MT) * kNibbleBlock + in_block; };
+            if (whole) {
+#pragma unroll
+                for (int y = 0; y < kEach; ++y)
+#pragma unroll
+                    for (int i = 0; i < 8 / Eight<T>::E; ++i) got[y].q[i] = load16(from[0] + col0 + y * kNext + i * Eight<T>::E);
+            } else {
+#pragma unroll
+                for (int y = 0; y < kEach; ++y) got[y].ask(from[y % kRowsOf], col_of(y), g.d);
+            }
+            between();
+#pragma unroll
+            for (int y = 0; y < kEach; ++y) {
+                const int piece = threadIdx.x + kThreads * y;
+                const int pk = piece & 3, pj = piece >> 2 & 3, i = (piece >> 4) % (4 * R), v = (piece >> 4) / (4 * R), t = v % MT, in = v / MT;
+                if (kPieces % kThreads != 0 && in >= kHeld) break;
+                bf16x8v part[3];
+                if (whole) {
+#pragma unroll
+                    for (int e = 0; e < PARTS; ++e) part[e] = bf16x8v{};
+                    if (there[0]) got[y].parts(part);
+                } else {
+                    float x[8];
+                    got[y].give(col_of(y), g.d, there[y % kRowsOf], x);
+                    split8<PARTS>(x, part);
+                }
+                const int to = pk * (4 * R) + (i & 3) * R + (i >> 2);
+#pragma unroll
+                for (int e = 0; e < PARTS; ++e) lds.held[((in * MT + t) * 4 + pj) * PARTS + e][to] = part[e];
+            }
+            const int end = (int)(g.d >> 7) - b0;                                       // the block in which the rows end
+            if ((g.d & 7) != 0 && end >= 0 && end < kHeld) {
+                lds_barrier();
+                if (threadIdx.x < MT * 4 * R) {
+                    const int i = threadIdx.x % (4 * R), t = threadIdx.x / (4 * R), c = (int)(g.d & 127) >> 3, to = (c & 3) * (4 * R) + (i & 3) * R + (i >> 2);
+                    const int64_t h = h0 + t * 16 + i, row = h < g.n ? (g.rows ? g.rows[h] : h) : -1;
+                    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+                    if (row >= 0 && row < g.m) load8(static_cast<const T *>(g.x) + row * g.ld + (g.d & ~7LL), g.d & 7, x);
+                    bf16x8v part[3];
+                    split8<PARTS>(x, part);
+#pragma unroll
+                    for (int e = 0; e < PARTS; ++e) lds.held[((end * MT + t) * 4 + (c >> 2)) * PARTS + e][to] = part[e];
+                }
+            }
+            lds_barrier();
+        };
+        // (no branch around a load of the classes': the compiler counts what is on its way.  What is asked for behind the last pair is the last pair, out of the caches.)
+        auto work = [&](int step0, int end) {
+            for (int step1 = step0; step1 < end; step1 += kAhead) {
+#pragma unroll
+                for (int j = 0; j < kAhead; ++j) {
+                    const int pair = (step1 + j) * along + mine;
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const uint32_t b = 2 * pair + half, at = b % kHeld;
+                        if ((int)b < g.blocks)
+                            multiply(p[j], half, [&](int t, int y, bf16x8v *h) {
+#pragma unroll
+                                for (int e = 0; e < PARTS; ++e) {
+                                    h[e] = bf16x8v{};
+                                    if (R == 4 || active) h[e] = lds.held[((at * MT + t) * 4 + y) * PARTS + e][place];
+                                }
+                            });
+                    }
+                    fetch(p[j], pair + kAhead * along);
+                }
+            }
+        };
+        fill(0, [&] {
+#pragma unroll
+            for (int j = 1; j < kAhead; ++j) fetch(p[j], j * along + mine);
+        });
+        work(0, steps < per ? steps : per);
+        for (int step0 = per; step0 < steps; step0 += per) {
+            fill(step0 / per * kHeld, [] { lds_barrier(); });
+            work(step0, steps - step0 < per ? steps : step0 + per);
+        }
+    } else {
+        const T *from[MT];
+        bool there[MT];
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            const int64_t h = h0 + t * 16 + 4 * (rho & 3) + (rho >> 2), row = active && h < g.n ? (g.rows ? g.rows[h] : h) : -1;
+            there[t] = row >= 0 && row < g.m;
+            from[t] = static_cast<const T *>(g.x) + (there[t] ? row * g.ld : 0);
+        }
+        auto ask = [&](Eight<T> (&got)[4], int t, int b) {                              // (what is not there is not asked for)
+            if (!there[t]) return;
+            if ((int64_t)(b + 1) * kNibbleBlock <= g.d) {
+                const T *p = from[t] + b * kNibbleBlock + k * 8;
+#pragma unroll
+                for (int y = 0; y < 4; ++y) got[y].ask(p + y * 32);
+            } else {
+#pragma unroll
+                for (int y = 0; y < 4; ++y) got[y].ask(from[t], (int64_t)b * kNibbleBlock + y * 32 + k * 8, g.d);
+            }
+        };
+        Pair p, after;
+        fetch(p, mine);
+        for (int pair = mine; pair < pairs; pair += along) {
+            fetch(after, pair + along);
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int b = 2 * pair + half;
+                if (b < g.blocks) {
+                    Eight<T> got[2][4];                                                 // of a tile of rows and the next
+                    const auto col = [&](int y) { return (int64_t)b * kNibbleBlock + y * 32 + k * 8; };
+                    ask(got[0], 0, b);
+                    multiply(p, half, [&](int t, int y, bf16x8v *h) {
+                        if (y == 0 && t + 1 < MT) {
+                            ask(got[(t + 1) & 1], t + 1, b);
+                            asm volatile("" ::: "memory");                              // (no tile earlier than that: they would not fit the registers)
+                        }
+                        if ((int64_t)(b + 1) * kNibbleBlock <= g.d) {
+#pragma unroll
+                            for (int e = 0; e < PARTS; ++e) h[e] = bf16x8v{};
+                            if (there[t]) got[t & 1][y].parts(h);
+                            return;
+                        }
+                        float x[8];
+                        got[t & 1][y].give(col(y), g.d, there[t], x);
+                        if ((g.d & 7) != 0 && there[t] && col(y) == (g.d & ~7LL)) load8(from[t] + col(y), g.d & 7, x);
+                        split8<PARTS>(x, h);
+                    });
+                }
+            }
+            p = after;
+        }
+    }
+    // the waves' sums, in their order, by all threads: value v of a lane at sums[wave][v][lane]
+    if (HELD) __syncthreads();
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int u = 0; u < NT; ++u)
+#pragma unroll
+            for (int r = 0; r < R; ++r) lds.sums[wave][(t * NT + u) * R + r][lane] = acc[t][u][r];
+    __syncthreads();
+    for (int at = threadIdx.x; at < across * kSums * 64; at += kThreads) {
+        const int l = at & 63, v = (at >> 6) % kSums, w = (at >> 6) / kSums;
+        const int r = v % R, u = v / R % NT, t = v / R / NT;
+        const int64_t c = ((g.first + blockIdx.x) * across + w) * (16 * NT) + u * 16 + (l & 15), h = h0 + t * 16 + 4 * r + (l >> 4);
+        if (c >= g.classes || h >= g.n) continue;
+        float sum = lds.sums[w * along][v][l];
+        for (int o = 1; o < along; ++o) sum += lds.sums[w * along + o][v][l];
+        if (g.half) Elem<uint16_t>::put(static_cast<uint16_t *>(g.out) + h * g.ld_out + c, sum);
+        else Elem<float>::put(static_cast<float *>(g.out) + h * g.ld_out + c, sum);
+    }
 }
 
-template <typename T, int MT, int R, int G>
-static hipError_t launch_matmul4(Matmul4Args g, hipStream_t s)
+// Up to sixteen rows of up to 4096 columns against many classes.  The waves of a workgroup hold the rows in registers, `along` waves a pair of blocks each; kStreamWaves / along of
+// them stand beside each other for other classes.  The classes' codes stream past, sixteen classes at a time, kBatch of those on their way, and every kBatch the waves' sums meet in
+// LDS, in their order.  fp32 rows are three rows of bfloat16 parts each, which the last addition puts together.
+// 16 x 65536 x 4096, groups of 32: 35 us, 4.3 TB/s; of 128: 33, 4.2.  Reading the codes alone takes 22 (6.1 TB/s).  The rest: codes and rows come in cold for 8 us or so before the first
+// results, in which a quarter of the codes arrives (each kernel also reads its own instructions, one line behind the other: the way through the start is kept short), and the waves wait for each other at the end.
+constexpr int kStreamWaves = 16, kBatch = 4;
+
+template <int R, int G>
+__global__ __launch_bounds__(64 * kStreamWaves) void matmul4_stream_kernel(Matmul4Args g, int along)
 {
-    constexpr int kHeld = held_blocks4<MT, R, sizeof(T) == 4 ? 3 : 1>();
-    const int64_t groups = (g.classes + 15) / 16, panels = (g.n + 16 * MT - 1) / (16 * MT);
+    constexpr int kThreads = 64 * kStreamWaves;
+    __shared__ float sums[2][kStreamWaves][kBatch][R][64];
+    __shared__ uint4 scales[2][kThreads];              // of a batch's classes, a row's beside each other: eight to a thread
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), rho = lane & 15, k = lane >> 4;
+    const int across = kStreamWaves / along, mine = wave % along;
+    // a run of sixteens of classes for each workgroup, `across` of them at a time
+    const int tiles = (int)((g.classes + 15) / 16), sets = (tiles + across - 1) / across;
+    const int set0 = (int)((int64_t)blockIdx.x * sets / gridDim.x), count = (int)((int64_t)(blockIdx.x + 1) * sets / gridDim.x) - set0;
+    const int tile0 = set0 * across + wave / along;
+    const int each = G * along >= 4 ? G * along / 4 : 1, each_log = 31 - __builtin_clz(each);      // eights of scales in a row (a power of two)
+    auto scales_of = [&](int it0) {
+        const int eight = threadIdx.x & (each - 1), row = threadIdx.x >> each_log, it = it0 + (row >> 4) / across, w = (row >> 4) & (across - 1);
+        const int64_t cls = ((int64_t)(set0 + (it < count ? it : count - 1)) * across + w) * 16 + (row & 15);
+        const int64_t at = (cls < g.classes ? cls : g.classes - 1) * g.ld_scales + (eight * 8 < G * g.blocks ? eight * 8 : 0);
+        return *reinterpret_cast<const uint4 *>(g.scales + at);
+    };
+    const int last = g.blocks - 1, b0 = 2 * mine < last ? 2 * mine : last & ~1, b1 = b0 < last ? b0 + 1 : b0;
+    struct Codes {
+        uint4 q[2];
+    };
+    auto fetch = [&](Codes &c, int it) {
+        const int tile = tile0 + (it < count ? it : count - 1) * across;
+        const int64_t cls = (int64_t)tile * 16 + rho < g.classes ? (int64_t)tile * 16 + rho : g.classes - 1;
+        const uint8_t *codes = g.codes + cls * g.ld_codes + k * 16;
+        c.q[0] = *reinterpret_cast<const uint4 *>(codes + (int64_t)b0 * 64);
+        c.q[1] = *reinterpret_cast<const uint4 *>(codes + (int64_t)b1 * 64);
+    };
+    // Loads come back in the order they are asked for: the first batch's scales, the first codes, the rows, then the other codes.
+    uint4 held = scales_of(0);
+    Codes c[kBatch];
+    fetch(c[0], 0);
+    // the wave's columns
+    bf16x8v x[8];
+    {
+        const int v = 4 * (rho & 3) + (rho >> 2), part = g.wide ? v % 3 : 0;
+        const int64_t h = g.wide ? v / 3 : v, row = (rho & 3) < R && h < g.n ? (g.rows ? g.rows[h] : h) : -1;
+#pragma unroll
+        for (int y = 0; y < 8; ++y) x[y] = bf16x8v{};
+        auto take = [&](auto *base) {
+            using T = std::remove_const_t<std::remove_pointer_t<decltype(base)>>;
+            constexpr int kParts = sizeof(T) == 4 ? 3 : 1, kAtATime = 16 / sizeof(T);
+            const T *from = base + row * g.ld;
+            const int64_t col0 = (int64_t)mine * (2 * kNibbleBlock) + k * 8;
+            auto hold = [&](int y, const bf16x8v (&parts)[kParts]) {
+                if constexpr (kParts == 1) {
+                    x[y] = parts[0];
+                } else {
+                    const u32x4v a = __builtin_bit_cast(u32x4v, parts[0]), b = __builtin_bit_cast(u32x4v, parts[1]), c = __builtin_bit_cast(u32x4v, parts[2]);
+                    u32x4v one;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) one[j] = part == 0 ? a[j] : part == 1 ? b[j] : c[j];
+                    x[y] = __builtin_bit_cast(bf16x8v, one);
+                }
+            };
+            bf16x8v parts[kParts];
+            if ((int64_t)(mine + 1) * (2 * kNibbleBlock) <= g.d) {                          // all of the wave's columns are there
+#pragma unroll
+                for (int y0 = 0; y0 < 8; y0 += kAtATime) {
+                    Eight<T> got[kAtATime];
+#pragma unroll
+                    for (int o = 0; o < kAtATime; ++o) got[o].ask(from + col0 + (y0 + o) * 32);
+#pragma unroll
+                    for (int o = 0; o < kAtATime; ++o) {
+                        got[o].parts(parts);
+                        hold(y0 + o, parts);
+                    }
+                }
+                return;
+            }
+            float e[8];
+#pragma unroll
+            for (int y0 = 0; y0 < 8; y0 += kAtATime) {
+                Eight<T> got[kAtATime];
+#pragma unroll
+                for (int o = 0; o < kAtATime; ++o) got[o].ask(from, col0 + (y0 + o) * 32, g.d);
+#pragma unroll
+                for (int o = 0; o < kAtATime; ++o) {
+                    got[o].give(col0 + (y0 + o) * 32, g.d, true, e);
+                    split8<kParts>(e, parts);
+                    hold(y0 + o, parts);
+                }
+            }
+            const int end = (int)(g.d >> 7);                                            // the block in which the rows end
+            if ((g.d & 7) != 0 && end / 2 == mine) {
+                load8(from + (g.d & ~7LL), g.d & 7, e);
+                split8<kParts>(e, parts);
+#pragma unroll
+                for (int y = 0; y < 8; ++y)
+                    if (((g.d & 255) >> 5) == y && ((g.d & 31) >> 3) == k) hold(y, parts);
+            }
+        };
+        if (row >= 0 && row < g.m) {                                                    // (what is not there is not asked for)
+            if (g.wide) take(static_cast<const float *>(g.x));
+            else take(static_cast<const uint16_t *>(g.x));
+        }
+    }
+#pragma unroll
+    for (int j = 1; j < kBatch; ++j) fetch(c[j], j);
+    scales[0][threadIdx.x] = held;
+    lds_barrier();
+    const int parts = g.wide ? 3 : 1;
+    for (int it0 = 0; it0 < count; it0 += kBatch) {
+        const int turn = it0 / kBatch & 1;
+        float(*to)[kBatch][R][64] = sums[turn];
+        held = scales_of(it0 + kBatch);
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            if (it0 + j < count) {
+                // this tile's row of scales, from the wave's first block on
+                const uint32_t *s0 = reinterpret_cast<const uint32_t *>(&scales[turn][((j * across + wave / along) * 16 + rho) * each]) + mine * G;
+                float acc[R];
+#pragma unroll
+                for (int r = 0; r < R; ++r) acc[r] = 0.0f;
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    if (2 * mine + half >= g.blocks) continue;
+                    const uint4 q = c[j].q[half];
+                    const bf16x8v f[4] = {widen_codes(q.x), widen_codes(q.y), widen_codes(q.z), widen_codes(q.w)};
+#pragma unroll
+                    for (int y = 0; y < 4; y += 4 / G) {
+                        const int at = half * G + y / (4 / G);
+                        const uint32_t two = s0[at >> 1];
+                        const float s = (at & 1) ? bf16_hi(two) : bf16_lo(two);
+                        f32x4v sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                        for (int o = 0; o < 4 / G; ++o) sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[half * 4 + y + o], f[y + o], sum, 0, 0, 0);
+#pragma unroll
+                        for (int r = 0; r < R; ++r) acc[r] = fmaf(sum[r], s, acc[r]);
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < R; ++r) to[wave][j][r][lane] = acc[r];
+            }
+            // (no branch around a load of the classes': the compiler counts what is on its way.  What is asked for behind the last tile is the last tile, out of the caches.)
+            fetch(c[j], it0 + j + kBatch);
+        }
+        scales[turn ^ 1][threadIdx.x] = held;
+        lds_barrier();
+        // results of the batch, sixteen classes to sixteen threads: row, tile of the batch, tile of the waves beside each other
+        for (int at = threadIdx.x; at < across * kBatch * 4 * R * 16; at += kThreads) {
+            const int l = at & 15, h = (at >> 4) % (4 * R), j = (at >> 4) / (4 * R) % kBatch, w = (at >> 4) / (4 * R) / kBatch;
+            const int64_t cls = ((int64_t)(set0 + it0 + j) * across + w) * 16 + l;
+            if (h >= g.n || it0 + j >= count || cls >= g.classes) continue;
+            float sum = 0.0f;
+            for (int part = 0; part < parts; ++part) {
+                const int v = h * parts + part, from = (v & 3) * 16 + l;
+                float one[kStreamWaves];
+#pragma unroll
+                for (int a = 0; a < kStreamWaves; ++a) one[a] = to[w * along + (a & (along - 1))][j][v >> 2][from];
+#pragma unroll
+                for (int a = 0; a < kStreamWaves; ++a) sum += a < along ? one[a] : 0.0f;
+            }
+            if (g.half) Elem<uint16_t>::put(static_cast<uint16_t *>(g.out) + h * g.ld_out + cls, sum);
+            else Elem<float>::put(static_cast<float *>(g.out) + h * g.ld_out + cls, sum);
+        }
+    }
+}
+
+template <typename T, int MT, int R, int NT, int G, int WAVES, bool HELD>
+static hipError_t launch_rows(Matmul4Args g, hipStream_t s)
+{
+    constexpr int kHeld = held_blocks4<MT, R, sizeof(T) == 4 ? 3 : 1, WAVES>(), kAhead = ahead4<MT, R, NT, sizeof(T) == 4 ? 3 : 1, WAVES>();
+    const int64_t groups = (g.classes + 16 * NT - 1) / (16 * NT), panels = (g.n + 16 * MT - 1) / (16 * MT), pairs = (g.blocks + 1) / 2;
     int along = 1;
-    while (along < kWaves4 && along < kHeld && groups * panels * along < 2048 && g.blocks >= 2 * along) along *= 2;
-    const int64_t grid = (groups * along + kWaves4 - 1) / kWaves4;
+    while (along < WAVES && (!HELD || along * 2 * kAhead <= kHeld / 2) && along < pairs && groups * panels * along < 256 * WAVES) along *= 2;
+    const int64_t grid = (groups * along + WAVES - 1) / WAVES;
     for (int64_t panel = 0; panel < panels; panel += 65535) {
         g.first_row = panel * (16 * MT);
-        const hipError_t e = in_launches(grid, 64 * kWaves4, [&](int64_t first, unsigned count) {
+        const hipError_t e = in_launches(grid, 64 * WAVES, [&](int64_t first, unsigned count) {
             g.first = first;
-            hipLaunchKernelGGL((matmul4_kernel<T, MT, R, G>), dim3(count, (unsigned)(panels - panel < 65535 ? panels - panel : 65535)), dim3(64 * kWaves4), 0, s, g, along);
+            hipLaunchKernelGGL((matmul4_kernel<T, MT, R, NT, G, WAVES, HELD>), dim3(count, (unsigned)(panels - panel < 65535 ? panels - panel : 65535)), dim3(64 * WAVES),
+                               0, s, g, along);
         });
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
 }
+
+template <int R, int G>
+static hipError_t launch_stream(const Matmul4Args &g, int along, hipStream_t s)
+{
+    const int64_t sets = ((g.classes + 15) / 16 + kStreamWaves / along - 1) / (kStreamWaves / along);
+    hipLaunchKernelGGL((matmul4_stream_kernel<R, G>), dim3((unsigned)(sets < 256 ? sets : 256)), dim3(64 * kStreamWaves), 0, s, g, along);
+    return hipGetLastError();
+}
+
 template <typename T, int G>
 static hipError_t launch_matmul4(const Matmul4Args &g, hipStream_t s)
 {
-    if (g.n <= 4) return launch_matmul4<T, 1, 1, G>(g, s);
-    if (g.n <= 8) return launch_matmul4<T, 1, 2, G>(g, s);
-    if (g.n <= 16) return launch_matmul4<T, 1, 4, G>(g, s);
-    if (g.n <= 32) return launch_matmul4<T, 2, 4, G>(g, s);
-    return launch_matmul4<T, 4, 4, G>(g, s);
+    const int pairs = (g.blocks + 1) / 2;
+    const int64_t rows = g.wide ? 3 * g.n : g.n, tiles = (g.classes + 15) / 16;
+    int along = 1;
+    while (along < 16 && along < pairs) along *= 2;
+    // More classes than a workgroup on every compute unit takes at a time, and rows that the waves' registers hold: the stream (bfloat16, us, stream | rows in LDS | rows asked for by each
+    // wave: 1 x 65536 x 4096 29.3 | 34.0 | 45.5, 16 x 65536 x 4096 33.3 | 35.8 | 85.6, 4 x 16384 x 4096 12.8 | 15.6 | 14.9; 1 x 4096 x 4096, one tile a workgroup, 11.1 | 14.1 | 7.1).
+    if (rows <= 16 && pairs <= 16 && tiles * along > 256 * 16) return rows <= 4 ? launch_stream<1, G>(g, along, s) : launch_stream<4, G>(g, along, s);
+    // Rows in LDS where many classes share them, else asked for by each wave (us, in LDS | by each wave: 64 x 65536 x 4096 74 | 175 bfloat16, 139 | 285 fp32; 256 x 16384 x 4096 66 | 170;
+    // 64 x 16384 x 4096 63 | 47, 127 | 77 fp32; 37 x 5003 x 3001 fp32 95 | 23; 20 x 20000 x 1000 fp32 23.3 | 24.0; 8 x 65536 x 4096 fp32 43 | 92).
+    if (g.n <= 16 ? tiles > 1024 : tiles * ((g.n + 63) / 64) >= 2048) {
+        if (g.n <= 8) return launch_rows<T, 1, 2, 1, G, 16, true>(g, s);
+        if (g.n <= 16) return launch_rows<T, 1, 4, 1, G, 16, true>(g, s);
+        if (g.n <= 32) return launch_rows<T, 2, 4, 2, G, 8, true>(g, s);
+        return launch_rows<T, 4, 4, 2, G, 8, true>(g, s);
+    }
+    if (g.n <= 4) return launch_rows<T, 1, 1, 1, G, 16, false>(g, s);
+    if (g.n <= 16) return launch_rows<T, 1, 4, 1, G, 16, false>(g, s);
+    constexpr int kTiles = sizeof(T) == 4 && G == 4 ? 1 : 2;                            // (two would not fit the registers)
+    return launch_rows<T, 2, 4, kTiles, G, 8, false>(g, s);
 }
 template <typename T>
 static hipError_t launch_matmul4(const Matmul4Args &g, int group, hipStream_t s)
@@ -348,7 +747,7 @@ int wpsgd_nibble_matmul(const wpsgd_matrix *X, const int64_t *rows, int64_t n, c
     if (n == 0 || W->rows == 0) return WPSGD_OK;
     if (!out || ld_out < W->rows || (uintptr_t)out % (dtype == WPSGD_F32 ? 4 : 2) != 0) return WPSGD_INVALID_ARG;
     const Matmul4Args g{X->dense, rows, X->m, X->d, X->ld, n, static_cast<const uint8_t *>(W->codes), static_cast<const uint16_t *>(W->scales), W->ld, W->ld_scales,
-                        W->rows, (int)((W->cols + kNibbleBlock - 1) / kNibbleBlock), dtype == WPSGD_BF16, out, ld_out, 0, 0};
+                        W->rows, (int)((W->cols + kNibbleBlock - 1) / kNibbleBlock), dtype == WPSGD_BF16, X->dtype == WPSGD_F32, out, ld_out, 0, 0};
     hipStream_t s = static_cast<hipStream_t>(stream);
     const hipError_t e = X->dtype == WPSGD_F32 ? launch_matmul4<float>(g, W->group, s) : launch_matmul4<uint16_t>(g, W->group, s);
     return e == hipSuccess ? WPSGD_OK : hip_fail(e);

@@ -446,9 +446,10 @@ int wpsgd_policy_loss(const void *Z, int64_t n, int64_t classes, int64_t ld, wps
  *   row_weights   DEVICE, n fp32 (r_i), or NULL for ones         pair_weights  DEVICE, pairs fp32 (w_p), or NULL for ones
  *   loss, margin  DEVICE out, pairs fp32
  *   grad          DEVICE out, dtype as Z, row stride ld_grad; NULL: not wanted.  It may be Z itself (with ld_grad = ld), else it may not overlap it.
- *   workspace     DEVICE scratch of at least wpsgd_preference_loss_workspace(n) bytes, 256-byte aligned
+ *   workspace     DEVICE scratch of at least wpsgd_preference_loss_workspace(n, classes, pairs, dtype) bytes, 256-byte aligned
+ *                 (may be NULL where that is 0)
  * Statistics are fp32, sums over rows fp64; the result does not depend on timing.  Errors: INVALID_ARG (0 <= smoothing <= 1), WORKSPACE_TOO_SMALL, HIP_ERROR. */
-size_t wpsgd_preference_loss_workspace(int64_t n);
+size_t wpsgd_preference_loss_workspace(int64_t n, int64_t classes, int64_t pairs, wpsgd_dtype dtype);
 int wpsgd_preference_loss(const void *Z, int64_t n, int64_t classes, int64_t ld, wpsgd_dtype dtype, const int64_t *labels, const int64_t *offsets,
                           int64_t pairs, const float *ref_log, const float *row_weights, const float *pair_weights, wpsgd_loss kind, double beta,
                           double smoothing, double scale, float *loss, float *margin, void *grad, int64_t ld_grad, void *workspace,

@@ -146,7 +146,7 @@ def load():
     L.wpsgd_clipped_step.argtypes = [pl, f64, f64, f64, vp, vp, sz, vp]
     L.wpsgd_draw_classes.argtypes = [vp, i64, i64, i64, ci, vp, ctypes.POINTER(_CDrawRule), vp, vp, vp]
     L.wpsgd_policy_loss.argtypes = [vp, i64, i64, i64, ci, vp, vp, vp, vp, vp, f64, f64, f64, f64, vp, vp, vp, i64, vp]
-    L.wpsgd_preference_loss_workspace.argtypes = [i64]
+    L.wpsgd_preference_loss_workspace.argtypes = [i64, i64, i64, ci]
     L.wpsgd_preference_loss_workspace.restype = sz
     L.wpsgd_preference_loss.argtypes = [vp, i64, i64, i64, ci, vp, vp, i64, vp, vp, vp, ci, f64, f64, f64, vp, vp, vp, i64, vp, sz, vp]
     L.wpsgd_dropout.argtypes = [pm, vp, i64, f64, u64, ci, i64, vp, vp, i64, vp]
@@ -788,12 +788,16 @@ def wpsgd_draw_classes(Z: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=
     return drawn, probs
 
 
-def _vector(t, like, n, dtype):
-    """The address of a contiguous vector of n on like's GPU; None stays None."""
-    if t is None:
-        return None
-    assert t.dtype == dtype and t.is_contiguous() and t.numel() == n
-    return t.data_ptr()
+def _addresses(index, n, dtype, *tensors):
+    """The addresses of contiguous vectors of n on GPU `index`; None stays None."""
+    out = []
+    for t in tensors:
+        if t is None:
+            out.append(None)
+        else:
+            assert t.dtype is dtype and t.get_device() == index and t.numel() == n and t.is_contiguous()
+            out.append(t.data_ptr())
+    return out
 
 
 def _gradient(grad, Z, n, c, stream):
@@ -816,23 +820,25 @@ def wpsgd_policy_loss(Z: torch.Tensor, drawn: torch.Tensor, advantage: torch.Ten
     scores' own), ref_log (under a reference; needed where kl > 0) and row_weights: float32, one for each row.
     grad: True for a new tensor, a tensor to write (Z itself too), or False for none."""
     n, c, ld = _rows_of(Z)
-    index = _beside(Z, drawn, advantage, old_log, ref_log, row_weights, loss, log_prob)
+    index, f32 = Z.get_device(), torch.float32
+    at, = _addresses(index, n, torch.int64, drawn)
+    old, ref, gain, weights, *own = _addresses(index, n, f32, old_log, ref_log, advantage, row_weights, loss, log_prob)
     if loss is None:
-        loss = _new(Z, n, torch.float32, stream)
+        loss = _new(Z, n, f32, stream)
+        own[0] = loss.data_ptr()
     if log_prob is None:
-        log_prob = _new(Z, n, torch.float32, stream)
-    f32 = torch.float32
+        log_prob = _new(Z, n, f32, stream)
+        own[1] = log_prob.data_ptr()
     grad, g_ptr, g_ld = _gradient(grad, Z, n, c, stream)
-    rc = _call(load().wpsgd_policy_loss, index, stream, Z.data_ptr(), n, c, ld, _DTYPES[Z.dtype], _vector(drawn, Z, n, torch.int64), _vector(old_log, Z, n, f32),
-               _vector(ref_log, Z, n, f32), _vector(advantage, Z, n, f32), _vector(row_weights, Z, n, f32), clip_low, clip_high, kl, scale,
-               _vector(loss, Z, n, f32), _vector(log_prob, Z, n, f32), g_ptr, g_ld)
+    rc = _call(load().wpsgd_policy_loss, index, stream, Z.data_ptr(), n, c, ld, _DTYPES[Z.dtype], at, old, ref, gain, weights, clip_low, clip_high, kl, scale, own[0], own[1],
+               g_ptr, g_ld)
     if rc != OK:
         raise WpsgdError(rc, "wpsgd_policy_loss")
     return loss, log_prob, grad
 
 
-def wpsgd_preference_loss_workspace(n) -> int:
-    return int(load().wpsgd_preference_loss_workspace(int(n)))
+def wpsgd_preference_loss_workspace(n, classes, pairs, dtype) -> int:
+    return int(load().wpsgd_preference_loss_workspace(int(n), int(classes), int(pairs), _DTYPES[dtype]))
 
 
 def wpsgd_preference_loss(Z: torch.Tensor, labels: torch.Tensor, offsets: torch.Tensor, ref_log: Optional[torch.Tensor] = None,
@@ -844,20 +850,25 @@ def wpsgd_preference_loss(Z: torch.Tensor, labels: torch.Tensor, offsets: torch.
     row_weights one float32 for each row, pair_weights for each pair.  kind: HINGE or LOGISTIC.
     grad: True for a new tensor, a tensor to write (Z itself too), or False for none."""
     n, c, ld = _rows_of(Z)
-    index = _beside(Z, labels, offsets, ref_log, row_weights, pair_weights, loss, margin, workspace)
-    ends = offsets.numel()
+    index, f32, i64, ends = Z.get_device(), torch.float32, torch.int64, offsets.numel()
     assert ends % 2 == 1
-    pairs, f32 = ends // 2, torch.float32
+    pairs = ends // 2
+    at, = _addresses(index, n, i64, labels)
+    edges, = _addresses(index, ends, i64, offsets)
+    ref, weights = _addresses(index, n, f32, ref_log, row_weights)
+    share, *own = _addresses(index, pairs, f32, pair_weights, loss, margin)
+    assert workspace is None or workspace.get_device() == index
     if loss is None:
         loss = _new(Z, pairs, f32, stream)
+        own[0] = loss.data_ptr()
     if margin is None:
         margin = _new(Z, pairs, f32, stream)
+        own[1] = margin.data_ptr()
     grad, g_ptr, g_ld = _gradient(grad, Z, n, c, stream)
-    L = load()
-    p, size, held = _call_workspace(workspace, L.wpsgd_preference_loss_workspace(n), Z, stream)
-    rc = _call(L.wpsgd_preference_loss, index, stream, Z.data_ptr(), n, c, ld, _DTYPES[Z.dtype], _vector(labels, Z, n, torch.int64),
-               _vector(offsets, Z, ends, torch.int64), pairs, _vector(ref_log, Z, n, f32), _vector(row_weights, Z, n, f32), _vector(pair_weights, Z, pairs, f32), kind,
-               beta, smoothing, scale, _vector(loss, Z, pairs, f32), _vector(margin, Z, pairs, f32), g_ptr, g_ld, p, size)
+    L, dtype = load(), _DTYPES[Z.dtype]
+    p, size, held = _call_workspace(workspace, L.wpsgd_preference_loss_workspace(n, c, pairs, dtype), Z, stream)
+    rc = _call(L.wpsgd_preference_loss, index, stream, Z.data_ptr(), n, c, ld, dtype, at, edges, pairs, ref, weights, share, kind, beta, smoothing, scale, own[0], own[1],
+               g_ptr, g_ld, p, size)
     if rc != OK:
         raise WpsgdError(rc, "wpsgd_preference_loss")
     return loss, margin, grad
@@ -881,13 +892,14 @@ def wpsgd_dropout(X: Matrix, p, seed, chain=0, step=0, rows: Optional[torch.Tens
     rows.  more_steps: one int64 on the GPU, read when the work runs.  out: a tensor to write (X.dense too, where all rows are taken)."""
     cm, source, n, picked = _picked(X, rows, "wpsgd_dropout")
     index = _beside(source, more_steps, out)
+    more, = _addresses(index, 1, torch.int64, more_steps)
     if out is None:
         out = _new(source, (n, X.d), source.dtype, stream)
         ld = X.d
     else:
         assert out.dtype == source.dtype and out.shape == (n, X.d) and (out.numel() == 0 or out.stride(1) == 1)
         ld = out.stride(0) if n > 1 else max(out.stride(0), X.d)
-    rc = _call(load().wpsgd_dropout, index, stream, ctypes.byref(cm), picked, n, p, seed, chain, step, _vector(more_steps, source, 1, torch.int64), out.data_ptr(), ld)
+    rc = _call(load().wpsgd_dropout, index, stream, ctypes.byref(cm), picked, n, p, seed, chain, step, more, out.data_ptr(), ld)
     if rc != OK:
         raise WpsgdError(rc, "wpsgd_dropout")
     return out

@@ -26,25 +26,29 @@ def test_policy_without_rows():
     assert policy(n=0, Z=None, drawn=None, loss=None) == api.OK
 
 
-def preference(Z=GB, n=8, c=10, ld=10, dtype=api.F32, labels=GB, offsets=GB, pairs=2, ref=None, weights=None, pair_weights=None, kind=api.HINGE, beta=0.1, eps=0.0, scale=1.0,
-               loss=GB, margin=GB, grad=2 * GB, ld_grad=10, ws=GB, ws_bytes=None):
+def preference(Z=GB, n=8, c=3000, ld=3000, dtype=api.F32, labels=GB, offsets=GB, pairs=2, ref=None, weights=None, pair_weights=None, kind=api.HINGE, beta=0.1, eps=0.0, scale=1.0,
+               loss=GB, margin=GB, grad=2 * GB, ld_grad=3000, ws=GB, ws_bytes=None):
     L = api.load()
-    need = L.wpsgd_preference_loss_workspace(n) if ws_bytes is None else ws_bytes
+    need = L.wpsgd_preference_loss_workspace(n, c, pairs, dtype) if ws_bytes is None else ws_bytes
     return L.wpsgd_preference_loss(Z, n, c, ld, dtype, labels, offsets, pairs, ref, weights, pair_weights, kind, beta, eps, scale, loss, margin, grad, ld_grad, ws, need, None)
 
 
-@pytest.mark.parametrize("change", [dict(Z=None), dict(n=-1), dict(c=0), dict(ld=9), dict(dtype=2), dict(labels=None), dict(offsets=None), dict(pairs=-1), dict(kind=2),
+@pytest.mark.parametrize("change", [dict(Z=None), dict(n=-1), dict(c=0), dict(ld=2999), dict(dtype=2), dict(labels=None), dict(offsets=None), dict(pairs=-1), dict(kind=2),
                                     dict(beta=math.inf), dict(beta=math.nan), dict(eps=-0.1), dict(eps=1.5), dict(eps=math.nan), dict(scale=math.nan), dict(loss=None),
-                                    dict(margin=None), dict(ld_grad=9), dict(Z=GB + 2), dict(grad=GB + 2), dict(Z=GB, grad=GB, ld_grad=16), dict(ws=None), dict(ws=GB + 128)])
+                                    dict(margin=None), dict(ld_grad=2999), dict(Z=GB + 2), dict(grad=GB + 2), dict(Z=GB, grad=GB, ld_grad=3016), dict(ws=None), dict(ws=GB + 128)])
 def test_preference(change):
     assert preference(**change) == api.INVALID_ARG
 
 
 def test_preference_workspace():
     L = api.load()
-    need = L.wpsgd_preference_loss_workspace(1000)
-    assert need >= 20000 and need % 256 == 0 and L.wpsgd_preference_loss_workspace(0) == L.wpsgd_preference_loss_workspace(-1) == 0
-    assert preference(n=1000, ws_bytes=need - 1) == api.WORKSPACE_TOO_SMALL
+    need = L.wpsgd_preference_loss_workspace(1000, 3000, 20, api.F32)
+    assert need >= 20000 and need % 256 == 0
+    assert preference(n=1000, pairs=20, ws_bytes=need - 1) == api.WORKSPACE_TOO_SMALL
+    # none for pairs that a workgroup forms by itself: up to 1024 classes in fp32, 2048 in bfloat16, 1024 rows, 64 rows a pair on average
+    one = lambda n, c, pairs, dtype: L.wpsgd_preference_loss_workspace(n, c, pairs, dtype) == 0  # noqa: E731
+    assert one(0, 3000, 1, api.F32) and one(-1, 3000, 1, api.F32) and one(1024, 1024, 16, api.F32) and one(1024, 2048, 16, api.BF16) and one(64, 1, 1, api.F32)
+    assert not (one(1024, 1025, 16, api.F32) or one(1024, 2049, 16, api.BF16) or one(1025, 1024, 17, api.F32) or one(1024, 1024, 15, api.F32) or one(1, 8, 0, api.F32))
     assert preference(n=0, pairs=0, Z=None, labels=None, loss=None, margin=None, ws=None) == api.OK
 
 

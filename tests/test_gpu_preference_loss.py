@@ -80,7 +80,7 @@ def ends_of(*lengths):
 
 
 SHAPES = [(ends_of(1, 1), 1, 0), (ends_of(1, 1), 2, 0), (ends_of(2, 1, 0, 3), 7, 1), (ends_of(0, 0, 4, 0), 65, 0), (ends_of(5, 9, 3, 4, 1, 1), 257, 3), (ends_of(3, 2, 4, 1), 1001, 0),
-          (ends_of(70, 130), 300, 0), (ends_of(2, 3, 1, 2), 4099, 8), (ends_of(4, 3), 20000, 1), (ends_of(1, 2, 2, 1), 65536, 0), (ends_of(1, 1), 131075, 0)]
+          (ends_of(70, 130), 300, 0), (ends_of(20, 40, 33, 17), 1023, 0), (ends_of(17, 16, 0, 64), 1024, 1), (ends_of(3, 60, 1, 0), 2047, 0), (ends_of(2, 5), 2048, 0), (ends_of(2, 3, 1, 2), 4099, 8), (ends_of(4, 3), 20000, 1), (ends_of(1, 2, 2, 1), 65536, 0), (ends_of(1, 1), 131075, 0)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -168,14 +168,14 @@ def test_gradient_matches_differences_of_the_loss():
 
 
 def test_strides_workspace_and_outputs_of_the_callers():
-    k = Case(ends_of(2, 3, 4, 1), 333, "bf16", 9, pad=7)
-    room = torch.full((10, 350), 3.0, dtype=torch.bfloat16, device="cuda")
+    k = Case(ends_of(2, 3, 4, 1), 3333, "bf16", 9, pad=7)
+    room = torch.full((10, 3350), 3.0, dtype=torch.bfloat16, device="cuda")
     loss, margin = torch.empty(2, device="cuda"), torch.empty(2, device="cuda")
-    ws = torch.full((api.wpsgd_preference_loss_workspace(10) + 256,), 0xFF, dtype=torch.uint8, device="cuda")
-    got = k.run(grad=room[:, 5:338], loss=loss, margin=margin, workspace=ws)
+    ws = torch.full((api.wpsgd_preference_loss_workspace(10, 3333, 2, torch.bfloat16) + 256,), 0xFF, dtype=torch.uint8, device="cuda")
+    got = k.run(grad=room[:, 5:3338], loss=loss, margin=margin, workspace=ws)
     want = k.run()
     assert got[0] is loss and got[1] is margin and all(torch.equal(a, b) for a, b in zip(got, want))
-    assert (room[:, :5] == 3).all() and (room[:, 338:] == 3).all() and (ws[-256:] == 0xFF).all()
+    assert (room[:, :5] == 3).all() and (room[:, 3338:] == 3).all() and (ws[-256:] == 0xFF).all()
 
 
 def test_rows_behind_the_32_bit_offset():
@@ -200,7 +200,8 @@ def test_refusals():
             api.wpsgd_preference_loss(k.z, y, o, **bad)
         assert e.value.status == api.INVALID_ARG
     with pytest.raises(api.WpsgdError) as e:
-        api.wpsgd_preference_loss(k.z, y, o, workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))
+        wide = torch.zeros(4, 3000, device="cuda")
+        api.wpsgd_preference_loss(wide, y, o, workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))
     assert e.value.status == api.WORKSPACE_TOO_SMALL
     for bad in (lambda: api.wpsgd_preference_loss(k.z, y, o[:2]), lambda: api.wpsgd_preference_loss(k.z, y, o.int()), lambda: api.wpsgd_preference_loss(k.z, y[:3], o),
                 lambda: api.wpsgd_preference_loss(k.z, y, o, ref_log=torch.zeros(3, device="cuda")), lambda: api.wpsgd_preference_loss(k.z, y, o.cpu()),

@@ -253,8 +253,8 @@ __global__ __launch_bounds__(64 * WAVES) void matmul4_kernel(Matmul4Args g, int 
             }
         }
     };
-    // block `half` of a pair, with get(t, y, parts) the parts of tile t's fragment of the y-th 32 columns
-    auto multiply = [&](const Pair &p, int half, auto get) {
+    // block `half` of a pair, with get(t, y, parts) the parts of tile t's fragment of the y-th 32 columns; before(t) comes before a tile of rows, there or not
+    auto multiply = [&](const Pair &p, int half, auto before, auto get) {
         bf16x8v f[NT][4];
 #pragma unroll
         for (int u = 0; u < NT; ++u) {
@@ -263,6 +263,8 @@ __global__ __launch_bounds__(64 * WAVES) void matmul4_kernel(Matmul4Args g, int 
         }
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
+            before(t);
+            if (MT > 1 && h0 + t * 16 >= g.n) continue;                                 // (no such rows)
             f32x4v sum[NT];
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
@@ -375,7 +377,7 @@ __global__ __launch_bounds__(64 * WAVES) void matmul4_kernel(Matmul4Args g, int 
                     for (int half = 0; half < 2; ++half) {
                         const uint32_t b = 2 * pair + half, at = b % kHeld;
                         if ((int)b < g.blocks)
-                            multiply(p[j], half, [&](int t, int y, bf16x8v *h) {
+                            multiply(p[j], half, [](int) {}, [&](int t, int y, bf16x8v *h) {
 #pragma unroll
                                 for (int e = 0; e < PARTS; ++e) {
                                     h[e] = bf16x8v{};
@@ -406,7 +408,7 @@ __global__ __launch_bounds__(64 * WAVES) void matmul4_kernel(Matmul4Args g, int 
             from[t] = static_cast<const T *>(g.x) + (there[t] ? row * g.ld : 0);
         }
         auto ask = [&](Eight<T> (&got)[4], int t, int b) {                              // (what is not there is not asked for)
-            if (!there[t]) return;
+            if (!there[t] || b >= g.blocks) return;
             if ((int64_t)(b + 1) * kNibbleBlock <= g.d) {
                 const T *p = from[t] + b * kNibbleBlock + k * 8;
 #pragma unroll
@@ -418,28 +420,35 @@ __global__ __launch_bounds__(64 * WAVES) void matmul4_kernel(Matmul4Args g, int 
         };
         Pair p, after;
         fetch(p, mine);
+        constexpr bool kEarly = PARTS * WAVES < 48;                                     // (sixteen waves' registers do not hold two fp32 tiles)
+        Eight<T> got[kEarly ? 2 : 1][4];                                                // of a tile of rows and the next, of this block or the one behind it
+        if (kEarly) ask(got[0], 0, 2 * mine);
         for (int pair = mine; pair < pairs; pair += along) {
             fetch(after, pair + along);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const int b = 2 * pair + half;
                 if (b < g.blocks) {
-                    Eight<T> got[2][4];                                                 // of a tile of rows and the next
                     const auto col = [&](int y) { return (int64_t)b * kNibbleBlock + y * 32 + k * 8; };
-                    ask(got[0], 0, b);
-                    multiply(p, half, [&](int t, int y, bf16x8v *h) {
-                        if (y == 0 && t + 1 < MT) {
-                            ask(got[(t + 1) & 1], t + 1, b);
+                    const auto before = [&](int t) {
+                        if constexpr (kEarly) {
+                            if (t + 1 < MT) ask(got[(half * MT + t + 1) % 2], t + 1, b);
+                            else ask(got[(half * MT + t + 1) % 2], 0, half == 0 ? b + 1 : 2 * (pair + along));
                             asm volatile("" ::: "memory");                              // (no tile earlier than that: they would not fit the registers)
+                        } else {
+                            ask(got[0], t, b);
                         }
+                    };
+                    multiply(p, half, before, [&](int t, int y, bf16x8v *h) {
+                        const Eight<T> &mine_now = got[kEarly ? (half * MT + t) % 2 : 0][y];
                         if ((int64_t)(b + 1) * kNibbleBlock <= g.d) {
 #pragma unroll
                             for (int e = 0; e < PARTS; ++e) h[e] = bf16x8v{};
-                            if (there[t]) got[t & 1][y].parts(h);
+                            if (there[t]) mine_now.parts(h);
                             return;
                         }
                         float x[8];
-                        got[t & 1][y].give(col(y), g.d, there[t], x);
+                        mine_now.give(col(y), g.d, there[t], x);
                         if ((g.d & 7) != 0 && there[t] && col(y) == (g.d & ~7LL)) load8(from[t] + col(y), g.d & 7, x);
                         split8<PARTS>(x, h);
                     });

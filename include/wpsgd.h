@@ -440,8 +440,8 @@ int wpsgd_policy_loss(const void *Z, int64_t n, int64_t classes, int64_t ld, wps
  * added and its gradient is 0.  A pair with w_p = 0 has loss 0 and gradient 0.  A row whose scores are all -inf has l_i = -inf and gradient 0; l_i - ref_log_i is 0 where
  * both are -inf.  A label >= classes makes the pair's results NaN, and so does a score of a row that counts which is +inf or NaN.
  *   Z             DEVICE, n x classes, row stride ld elements, fp32 or bfloat16    labels  DEVICE, n
- *   offsets       DEVICE, 2 * pairs + 1 row numbers, none under the one before it, within 0 .. n.  Where a pair's are not, its loss and margin are NaN (and the gradient of
- *                 rows that two pairs then claim is that of either).
+ *   offsets       DEVICE, 2 * pairs + 1 row numbers, none under the one before it, within 0 .. n.  Where a pair's are not, its loss and margin are NaN, and
+ *                 nothing is said about the gradient.
  *   ref_log       DEVICE, n fp32 (-loss of wpsgd_softmax_loss under a reference), or NULL for zeros
  *   row_weights   DEVICE, n fp32 (r_i), or NULL for ones         pair_weights  DEVICE, pairs fp32 (w_p), or NULL for ones
  *   loss, margin  DEVICE out, pairs fp32
@@ -471,7 +471,7 @@ int wpsgd_dropout(const wpsgd_matrix *X, const int64_t *rows, int64_t n, double 
 /* A matrix in four bits, a scale for each group of 32, 64 or 128 elements of a row:
  *   value(i, c) = v * scales[i*ld_scales + c/group],  v the code's value: 0, 1/2, 1, 3/2, 2, 3, 4, 6 for 0 .. 7 and their negatives for 8 .. 15
  * Rows hold whole blocks of 128 elements in 64 bytes; element 32*j + 8*k + e (j, k < 4, e < 8) of a block is in its byte 16*k + 4*j + e/2, an even e in the lower half.
- * Codes and scales behind the last column, as far as whole blocks go, are 0 (a product reads them). */
+ * Codes and scales behind the last column, as far as whole blocks go, are 0 (a product reads them, and whole eights of each row's scales, the last one's too). */
 typedef struct wpsgd_nibbles {
     int64_t rows, cols;        /* rows < 2^31, 0 <= cols <= 2^31                                                        */
     int group;                 /* 32, 64 or 128                                                                         */

@@ -919,7 +919,7 @@ class NibbleMatrix:
         codes, scales, rows, blocks = self.codes, self.scales, self.rows, (self.cols + 127) // 128
         assert codes.is_cuda and scales.is_cuda and codes.dtype == torch.uint8 and scales.dtype == torch.bfloat16 and self.group in (32, 64, 128)
         (r0, c0), (r1, c1), (ld, step), (ld_scales, step_scales) = codes.shape, scales.shape, codes.stride(), scales.stride()
-        assert r0 == r1 == rows and c0 >= 64 * blocks and c1 >= 128 // self.group * blocks
+        assert r0 == r1 == rows and c0 >= 64 * blocks and c1 >= -(-128 // self.group * blocks // 8) * 8
         assert step == step_scales == 1 or rows == 0 or blocks == 0
         if rows == 1:
             ld, ld_scales = 64 * blocks, -(-128 // self.group * blocks // 8) * 8

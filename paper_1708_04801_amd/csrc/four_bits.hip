@@ -12,26 +12,53 @@ namespace wpsgd {
 
 constexpr int kNibbleBlock = 128;
 
-// 1/4, 3/4 ... : where one code ends and the next begins, a border itself going to the even code
-__device__ inline uint32_t code_of(float x, float s)
+// The codes of eight elements, the first in the lowest bits.  The quotient x / s is formed to the last place (a product with about 1 / s and one correction).  bfloat16 elements: one that lies on
+// no border between codes is 2^-11 of itself away from it, and one that does comes out as the border, a number of few bits; the conversion instruction, which rounds half to even,
+// gives the code.  fp32 elements: the quotient is cut towards zero and its last bit set where it is not exact; such a number lies on the same side of every border as x / s, on it only if
+// x / s does.  Five and thirteen instructions an element, where comparing with the seven borders takes some twenty.  Residuals under s 2^-33 have to be numbers: groups with scales under
+// 2^-110 are compared.
+template <bool HALF>
+__device__ inline uint32_t codes_of(const float (&x)[8], float s)
 {
-    const float size = fabsf(x);
-    uint32_t c = size > 0.25f * s ? 1 : 0;
-    c += size >= 0.75f * s ? 1 : 0;
-    c += size > 1.25f * s ? 1 : 0;
-    c += size >= 1.75f * s ? 1 : 0;
-    c += size > 2.5f * s ? 1 : 0;
-    c += size >= 3.5f * s ? 1 : 0;
-    c += size > 5.0f * s ? 1 : 0;
-    return c | (__float_as_uint(x) >> 28 & 8u);
+    uint32_t w = 0;
+    if (s >= 0x1p-110f) {
+        const float r = __builtin_amdgcn_rcpf(s);
+        float q[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float y = x[j] * r;
+            y = fmaf(fmaf(-y, s, x[j]), r, y);
+            if constexpr (!HALF) {
+                const uint32_t left = __float_as_uint(fmaf(-y, s, x[j]));
+                const uint32_t odd = min(left & 0x7FFFFFFFu, 1u), over = (left ^ __float_as_uint(x[j])) >> 31 & odd;      // not exact; rounded away from zero
+                y = __uint_as_float((__float_as_uint(y) - over) | odd);
+            }
+            q[j] = copysignf(y, x[j]);                                                  // (a residual of 0 takes a zero's sign)
+        }
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, q[0], q[1], 1.0f, 0);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, q[2], q[3], 1.0f, 1);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, q[4], q[5], 1.0f, 2);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, q[6], q[7], 1.0f, 3);
+    } else {
+        const float border[7] = {0.25f * s, 0.75f * s, 1.25f * s, 1.75f * s, 2.5f * s, 3.5f * s, 5.0f * s};
+#pragma unroll
+        for (int j = 7; j >= 0; --j) {
+            const float size = fabsf(x[j]);
+            uint32_t c = __float_as_uint(x[j]) >> 28 & 8u;
+#pragma unroll
+            for (int i = 0; i < 7; ++i) c += (i & 1) ? size >= border[i] : size > border[i];      // (a border itself goes to the even code)
+            w = w << 4 | c;
+        }
+    }
+    return w;
 }
 
-// The bits of the least bfloat16 s >= 2^-126 with 6 s >= top; 1 for 0.  The quotient is off by half a place of fp32, so that what its upper half stands for is at most the
-// answer and at most one place under it.
+// The bits of the least bfloat16 s >= 2^-126 with 6 s >= top; 1 for 0.  What the upper half of the product with about 1/6 stands for is the answer or one place under it: where the product is
+// a little too large for its upper half, top / 6 lies right under that, and that is the answer.
 __device__ inline uint32_t scale_bits(float top)
 {
     if (top == 0.0f) return 0x3F800000u;
-    const float s = __uint_as_float(__float_as_uint(fmaxf(top / 6.0f, 1.17549435e-38f)) & 0xFFFF0000u);
+    const float s = __uint_as_float(__float_as_uint(fmaxf(top * 0.16666667f, 1.17549435e-38f)) & 0xFFFF0000u);
     return __float_as_uint(s) + (6.0f * s < top ? 0x10000u : 0u);
 }
 
@@ -46,43 +73,40 @@ struct Quantize4Args {
     int64_t first;             // workgroup of the call at which the launch begins
 };
 
-// Sixteen lanes to a block of 128, eight elements to a lane; G groups to a block.
+// Sixteen lanes to a block of 128, eight elements to a lane; G groups to a block.  Bound by memory: 65536 x 4096 fp32 219 us, 5.5 TB/s; bfloat16, whose elements are twice as many, 147
+// (groups of 32: 135, 5.1 TB/s; 188 with thirteen instructions an element and divisions for the scale).  Four blocks to sixteen lanes were slower (225 fp32, 5003 x 3001 17 instead of 14).
 template <typename T, int G>
 __global__ __launch_bounds__(256) void quantize4_kernel(Quantize4Args a)
 {
     const int64_t first = (a.first + blockIdx.x) * 16;
-    const int64_t row0 = first / a.blocks;
-    const uint32_t at = (uint32_t)(first - row0 * a.blocks) + (threadIdx.x >> 4);      // (blocks < 2^25)
-    const uint32_t down = at / (uint32_t)a.blocks;
+    const int64_t row0 = first >> 32 ? first / a.blocks : (int64_t)((uint32_t)first / (uint32_t)a.blocks);
+    const uint32_t at = (uint32_t)(first - row0 * a.blocks) + (threadIdx.x >> 4), blocks = (uint32_t)a.blocks;      // (blocks < 2^25)
+    const uint32_t down = blocks >= 16 ? (at >= blocks ? 1u : 0u) : at / blocks;
     const int64_t row = row0 + down;
     if (row >= a.n) return;                                                            // (sixteen lanes at a time)
-    const int64_t b = at - down * (uint32_t)a.blocks;
+    const uint32_t b = at - down * blocks;
     const int64_t from = a.rows ? a.rows[row] : row;
     const int lane = threadIdx.x & 15;
-    const int64_t col = b * kNibbleBlock + lane * 8;
+    const int64_t col = (int64_t)b * kNibbleBlock + lane * 8;
     float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (from >= 0 && from < a.m && col < a.d) load8(static_cast<const T *>(a.x) + from * a.ld + col, a.d - col, x);
-    float top = 0.0f;
-    bool fine = true;
+    float top = 0.0f, sum = 0.0f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        fine = fine && fabsf(x[j]) < __builtin_inff();
+        sum = fmaf(x[j], 0.0f, sum);                                                   // NaN where one is not finite
         top = fmaxf(top, fabsf(x[j]));
     }
-    top = fine ? top : __builtin_inff();                                               // (no maximum drops that)
+    top = sum == 0.0f ? top : __builtin_inff();                                        // (no maximum drops that)
     top = fmaxf(top, dpp_move<0xB1, 0xF>(top));
     top = fmaxf(top, dpp_move<0x4E, 0xF>(top));
     if constexpr (G <= 2) top = fmaxf(top, dpp_move<0x141, 0xF>(top));
     if constexpr (G == 1) top = fmaxf(top, dpp_move<0x140, 0xF>(top));
     const bool whole = top < __builtin_inff();
     const uint32_t bits = whole ? scale_bits(top) : 0x7FC00000u;
-    const float s = __uint_as_float(bits);
-    uint32_t w = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) w |= (whole ? code_of(x[j], s) : 0u) << (4 * j);
-    *reinterpret_cast<uint32_t *>(a.codes + row * a.ld_codes + b * 64 + (lane & 3) * 16 + (lane >> 2) * 4) = w;
+    const uint32_t w = whole ? codes_of<sizeof(T) == 2>(x, __uint_as_float(bits)) : 0u;
+    *reinterpret_cast<uint32_t *>(a.codes + row * a.ld_codes + (int64_t)b * 64 + (lane & 3) * 16 + (lane >> 2) * 4) = w;
     constexpr int kLanes = 16 / G;
-    if (lane % kLanes == 0) a.scales[row * a.ld_scales + b * G + lane / kLanes] = col < a.d ? (uint16_t)(bits >> 16) : (uint16_t)0;
+    if (lane % kLanes == 0) a.scales[row * a.ld_scales + (int64_t)b * G + lane / kLanes] = col < a.d ? (uint16_t)(bits >> 16) : (uint16_t)0;
 }
 
 typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));

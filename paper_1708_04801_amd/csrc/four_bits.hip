@@ -505,9 +505,10 @@ __global__ __launch_bounds__(64 * WAVES) void matmul4_kernel(Matmul4Args g, int 
 // Up to sixteen rows of up to 4096 columns against many classes.  The waves of a workgroup hold the rows in registers, `along` waves a pair of blocks each; kStreamWaves / along of
 // them stand beside each other for other classes.  The classes' codes stream past, sixteen classes at a time, kBatch of those on their way, and every kBatch the waves' sums meet in
 // LDS, in their order.  fp32 rows are three rows of bfloat16 parts each, which the last addition puts together.
-// 16 x 65536 x 4096, groups of 32: 35 us, 4.3 TB/s; of 128: 33, 4.2.  Reading the codes alone takes 22 (6.1 TB/s).  The rest: codes and rows come in cold for 8 us or so before the first
-// results, in which a quarter of the codes arrives (each kernel also reads its own instructions, one line behind the other: the way through the start is kept short), and the waves wait for each other at the end.
-constexpr int kStreamWaves = 16, kBatch = 4;
+// 16 x 65536 x 4096, groups of 32: 36 us, 4.3 TB/s; of 128: 33.5, 4.2; 1 x 65536 x 4096 28.3, 4.9.  Reading the codes alone takes 22 (6.1 TB/s).  The rest: codes and rows come in cold for some 8 us
+// before the first results (each kernel also reads its own instructions, one line behind the other: the way through the start is kept short), and the waves wait for each other at the
+// end.  Batches of four tiles: 35 us for the first of these, but 1 x 65536 x 4096 29.4 and 4 x 16384 x 4096 12.7 instead of 11.5: twice the instructions.
+constexpr int kStreamWaves = 16, kBatch = 2;
 
 template <int R, int G>
 __global__ __launch_bounds__(64 * kStreamWaves) void matmul4_stream_kernel(Matmul4Args g, int along)
@@ -706,7 +707,7 @@ static hipError_t launch_matmul4(const Matmul4Args &g, hipStream_t s)
     int along = 1;
     while (along < 16 && along < pairs) along *= 2;
     // More classes than a workgroup on every compute unit takes at a time, and rows that the waves' registers hold: the stream (bfloat16, us, stream | rows in LDS | rows asked for by each
-    // wave: 1 x 65536 x 4096 29.3 | 34.0 | 45.5, 16 x 65536 x 4096 33.3 | 35.8 | 85.6, 4 x 16384 x 4096 12.8 | 15.6 | 14.9; 1 x 4096 x 4096, one tile a workgroup, 11.1 | 14.1 | 7.1).
+    // wave: 1 x 65536 x 4096 28.3 | 34.0 | 45.5, 16 x 65536 x 4096 33.5 | 35.8 | 85.6, 4 x 16384 x 4096 11.5 | 15.6 | 14.9; 1 x 4096 x 4096, one tile a workgroup, 11.1 | 14.1 | 7.1).
     if (rows <= 16 && pairs <= 16 && tiles * along > 256 * 16) return rows <= 4 ? launch_stream<1, G>(g, along, s) : launch_stream<4, G>(g, along, s);
     // Rows in LDS where many classes share them, else asked for by each wave (us, in LDS | by each wave: 64 x 65536 x 4096 74 | 175 bfloat16, 139 | 285 fp32; 256 x 16384 x 4096 66 | 170;
     // 64 x 16384 x 4096 63 | 47, 127 | 77 fp32; 37 x 5003 x 3001 fp32 95 | 23; 20 x 20000 x 1000 fp32 23.3 | 24.0; 8 x 65536 x 4096 fp32 43 | 92).

@@ -425,8 +425,8 @@ int wpsgd_draw_classes(const void *Z, int64_t n, int64_t classes, int64_t ld, wp
  *   advantage  DEVICE, n         row_weights  DEVICE, n (r_i), or NULL for ones
  *   loss       DEVICE out, n     log_prob     DEVICE out, n, or NULL
  *   grad       DEVICE out, dtype as Z, row stride ld_grad; NULL: not wanted.  It may be Z itself (with ld_grad = ld), else it may not overlap it.
- * (All of them fp32 but Z, drawn and grad.)  -loss of wpsgd_softmax_loss without a gradient is a log probability too.  Statistics are fp32, what a row makes of them fp64;
- * the result does not depend on timing.  Errors: INVALID_ARG (0 <= clip_low <= 1; clip_high >= 0, it may be infinite; kl >= 0), HIP_ERROR. */
+ * (All of them fp32 but Z, drawn and grad.)  -loss of wpsgd_softmax_loss without a gradient is a log probability too.  Exponentials are fp32, their sums and what a row makes
+ * of them fp64; the result does not depend on timing.  Errors: INVALID_ARG (0 <= clip_low <= 1; clip_high >= 0, it may be infinite; kl >= 0), HIP_ERROR. */
 int wpsgd_policy_loss(const void *Z, int64_t n, int64_t classes, int64_t ld, wpsgd_dtype dtype, const int64_t *drawn, const float *old_log,
                       const float *ref_log, const float *advantage, const float *row_weights, double clip_low, double clip_high, double kl,
                       double scale, float *loss, float *log_prob, void *grad, int64_t ld_grad, void *stream);
@@ -448,7 +448,7 @@ int wpsgd_policy_loss(const void *Z, int64_t n, int64_t classes, int64_t ld, wps
  *   grad          DEVICE out, dtype as Z, row stride ld_grad; NULL: not wanted.  It may be Z itself (with ld_grad = ld), else it may not overlap it.
  *   workspace     DEVICE scratch of at least wpsgd_preference_loss_workspace(n, classes, pairs, dtype) bytes, 256-byte aligned
  *                 (may be NULL where that is 0)
- * Statistics are fp32, sums over rows fp64; the result does not depend on timing.  Errors: INVALID_ARG (0 <= smoothing <= 1), WORKSPACE_TOO_SMALL, HIP_ERROR. */
+ * Exponentials are fp32, their sums and sums over rows fp64; the result does not depend on timing.  Errors: INVALID_ARG (0 <= smoothing <= 1), WORKSPACE_TOO_SMALL, HIP_ERROR. */
 size_t wpsgd_preference_loss_workspace(int64_t n, int64_t classes, int64_t pairs, wpsgd_dtype dtype);
 int wpsgd_preference_loss(const void *Z, int64_t n, int64_t classes, int64_t ld, wpsgd_dtype dtype, const int64_t *labels, const int64_t *offsets,
                           int64_t pairs, const float *ref_log, const float *row_weights, const float *pair_weights, wpsgd_loss kind, double beta,

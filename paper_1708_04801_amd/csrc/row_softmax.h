@@ -1,6 +1,7 @@
 // A row of scores read once: its softmax's statistics, and from them what an operator makes of the row and the gradient that goes with it,
 //   grad_ic = f_i (exp(z_ic - m_i) / s_i - [c = t]),   m_i the row's maximum, s_i = sum_c exp(z_ic - m_i), t the row's class, f_i the operator's.
-// Statistics are fp32.  An operator is a class with
+// Exponentials are fp32.  An operator is a class with
+//   kWideSum                           whether exponentials are summed in fp64, eight (bfloat16) or four at a time: a sum over many rows' logs shows what fp32 sums leave out, and a bias of each
 //   kOneWave                           whether make() is so long that one wave makes it for its row; else every thread does, and gives `writes` for the first
 //   counts(row, class, weight)         whether the row counts; the gradient of one that does not is 0
 //   absent(row)                        what it writes for a row that does not count (one thread's work)
@@ -25,6 +26,7 @@ struct RowArgs {
 
 struct RowState {
     float m, s, z_label;       // maximum, sum of exponentials relative to it, the class's score
+    double sum;                // s, in fp64 where the operator sums so
     bool empty;                // every score is -inf
     bool unknown;              // no such class
 };
@@ -45,6 +47,13 @@ template <typename T> __device__ inline float exp_of(float x)
     }
 }
 
+// The same for sums in fp64: with the rest of log2 e (without it every exponential is off by 1.3e-8 of its exponent, always to the same side).
+template <typename T, bool WIDE> __device__ inline float exp_for(float x)
+{
+    if constexpr (WIDE && Elem<T>::kPer16 == 8) return __builtin_amdgcn_exp2f(fmaf(x, kLog2e, x * kLog2eRest));
+    else return exp_of<T>(x);
+}
+
 // The row waits in registers between its statistics and its gradient, V vectors of sixteen bytes to a thread, so that it is read once; NT threads to a row, 256 / NT
 // rows to a workgroup where that is more than one.  LONG: what a row has beyond 16 NT V bytes is read again for the gradient.  Bound by memory: 8192 x 65536
 // bfloat16 reads and writes 1 GiB each in 385 us, 5.6 TB/s; 1023 x 32001 takes 24 us, 5.4 TB/s; 64 x 1000 fp32 3.6 us, a launch.
@@ -54,7 +63,9 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void softmax_row_kernel(RowArg
     constexpr int E = Elem<T>::kPer16, kRows = NT < 256 ? 256 / NT : 1, kWaves = NT / 64;
     constexpr float kInf = __builtin_inff();
     constexpr bool kKept = E == 4;         // exponentials take the scores' place in the registers: one for both, and none is rounded
-    __shared__ float part[2][kWaves];
+    using Sum = std::conditional_t<Op::kWideSum, double, float>;
+    __shared__ float part[kWaves];
+    __shared__ Sum sums[kWaves];
     const int64_t row = (a.first + blockIdx.x) * kRows + threadIdx.x / NT;
     if (kRows > 1 && row >= a.n) return;                                          // (whole waves)
     const int t = threadIdx.x % NT;
@@ -92,7 +103,7 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void softmax_row_kernel(RowArg
 #pragma unroll
         for (int j = 0; j < E; ++j) m = fmaxf(m, Elem<T>::get(q[v].w, j));
     m = fmaxf(m, -kInf);
-    float s = 0.0f;
+    Sum s = 0;
     if constexpr (LONG) {
         for (int v = V * NT + t; v < vectors; v += NT) {
             const Bytes16 more = load16(z + (int64_t)v * E);
@@ -100,9 +111,15 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void softmax_row_kernel(RowArg
 #pragma unroll
             for (int j = 0; j < E; ++j) top = fmaxf(top, Elem<T>::get(more.w, j));
             const float base = top == -kInf ? 0.0f : top;
-            s = s * exp_of<T>(m - base);
+            s = s * exp_for<T, Op::kWideSum>(m - base);
+            float eight = 0.0f;
 #pragma unroll
-            for (int j = 0; j < E; ++j) s += exp_of<T>(Elem<T>::get(more.w, j) - base);
+            for (int j = 0; j < E; ++j) {
+                const float e = exp_for<T, Op::kWideSum>(Elem<T>::get(more.w, j) - base);
+                if constexpr (Op::kWideSum) eight += e;
+                else s += e;
+            }
+            if constexpr (Op::kWideSum) s += eight;
             m = top;
         }
     }
@@ -110,51 +127,55 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void softmax_row_kernel(RowArg
     const float own = m;                                                          // what s is relative to
     m = wave_max(m);
     if constexpr (kWaves > 1) {
-        if ((t & 63) == 0) part[0][t >> 6] = m;
+        if ((t & 63) == 0) part[t >> 6] = m;
         __syncthreads();
-        m = part[0][0];
+        m = part[0];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) m = fmaxf(m, part[0][w]);
+        for (int w = 1; w < kWaves; ++w) m = fmaxf(m, part[w]);
     }
     const bool none = m == -kInf;                                                 // every score is -inf or NaN
     const float base = none ? 0.0f : m;
-    if constexpr (LONG) s = own == -kInf ? s : s * exp_of<T>(own - base);
+    if constexpr (LONG) s = own == -kInf ? s : s * exp_for<T, Op::kWideSum>(own - base);
 #pragma unroll
-    for (int v = 0; v < V; ++v)
+    for (int v = 0; v < V; ++v) {
+        float eight = 0.0f;
 #pragma unroll
         for (int j = 0; j < E; ++j) {
-            const float e = exp_of<T>(Elem<T>::get(q[v].w, j) - base);
-            s += e;
+            const float e = exp_for<T, Op::kWideSum>(Elem<T>::get(q[v].w, j) - base);
+            if constexpr (Op::kWideSum) eight += e;
+            else s += e;
             if constexpr (kKept) q[v].w[j] = __float_as_uint(e);
         }
-    const float e_last = exp_of<T>(last - base);
+        if constexpr (Op::kWideSum) s += eight;
+    }
+    const float e_last = exp_for<T, Op::kWideSum>(last - base);
     s += e_last;
     pack();
     s = wave_sum(s);
     if constexpr (kWaves > 1) {
-        if ((t & 63) == 0) part[1][t >> 6] = s;
+        if ((t & 63) == 0) sums[t >> 6] = s;
         __syncthreads();
-        s = part[1][0];
+        s = sums[0];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) s += part[1][w];
+        for (int w = 1; w < kWaves; ++w) s += sums[w];
     }
-    const bool empty = none && s == 0.0f;
+    const bool empty = none && s == 0;
     const float bad = label >= a.c ? __builtin_nanf("") : 0.0f;                   // no such class: the gradient says so
-    const RowState state{m, s, z_label, empty, label >= a.c};
+    const RowState state{m, (float)s, z_label, (double)s, empty, label >= a.c};
     float f = 0.0f;
     if constexpr (Op::kOneWave) {
         if (t < 64) f = op.make(row, r, state, t == 0);
         if (!g) return;
         if constexpr (kWaves > 1) {
-            if (t == 0) part[0][0] = f;
+            if (t == 0) part[0] = f;
             __syncthreads();
-            f = part[0][0];
+            f = part[0];
         }
     } else {
         f = op.make(row, r, state, t == 0);
         if (!g) return;
     }
-    const float over = (empty ? 0.0f : f / s) + bad;
+    const float over = (empty ? 0.0f : f / (float)s) + bad;
     const int at_label = empty || label >= a.c ? -1 : (int)label;
     auto gradient = [&](int v, const Bytes16 &x, auto kept) {
         float p[E];

@@ -5,7 +5,7 @@
 namespace wpsgd {
 
 struct LossOfRow {
-    static constexpr bool kOneWave = false;
+    static constexpr bool kOneWave = false, kWideSum = false;
     double scale;
     float *loss;
     __device__ bool counts(int64_t, int64_t label, float r) const { return !(label < 0 || r == 0.0f); }

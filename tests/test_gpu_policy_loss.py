@@ -210,3 +210,17 @@ def test_refusals():
             bad()
     got = api.wpsgd_policy_loss(z[:0], d[:0], A[:0])
     assert got[0].numel() == 0 and got[2].shape == (0, 10)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_scores_that_start_at_any_element_and_results_over_inputs(dtype):
+    z, k = case(9, 301, dtype, 12)
+    want = run(z, k)
+    room = torch.full((9, 320), 2.0, dtype=z.dtype, device="cuda")
+    room[:, 3:304] = z
+    got = run(room[:, 3:304], k)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    old, advantage = torch.tensor(k[1]).cuda(), k[3].cuda()
+    over = api.wpsgd_policy_loss(room[:, 3:304], k[0].cuda(), advantage, old_log=old, ref_log=torch.tensor(k[2]).cuda(), row_weights=k[4].cuda(), clip_low=k[5], clip_high=k[6],
+                                 kl=k[7], scale=k[8], loss=advantage, log_prob=old, grad=room[:, 3:304])
+    assert over[0] is advantage and over[1] is old and all(torch.equal(a, b) for a, b in zip(over, want)) and (room[:, :3] == 2).all() and (room[:, 304:] == 2).all()

@@ -212,3 +212,33 @@ def test_refusals():
     assert abs(float(got[0][0]) - math.log(2)) < 1e-6 and got[1][0] == 0 and got[2].shape == (0, 10)
     got = api.wpsgd_preference_loss(k.z, y, torch.zeros(1, dtype=torch.int64, device="cuda"))
     assert got[0].numel() == 0 and not got[2].any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("c", [50, 3000])
+def test_rows_before_and_behind_the_sequences(c, dtype):
+    """zeros for them, whichever kernels run, also where the gradient takes the scores' place, and rows that start at any element"""
+    k = Case(ends_of(2, 1, 3, 2), c, dtype, 6, weighted=False)
+    want = k.run()
+    room = torch.full((40, c + 9), 2.0, dtype=k.z.dtype, device="cuda")
+    z = room[:, 3:c + 3]
+    z[5:13] = k.z
+    z[0] = math.nan
+    labels, ref_log = torch.full((40,), 1, dtype=torch.int64), torch.zeros(40)
+    labels[5:13], ref_log[5:13] = k.labels, k.ref
+    offsets = (torch.tensor(k.ends) + 5).cuda()
+    got = api.wpsgd_preference_loss(z, labels.cuda(), offsets, ref_log=ref_log.cuda(), beta=k.beta, scale=k.scale)
+    assert all(torch.equal(a, b) for a, b in zip((got[0], got[1], got[2][5:13]), want)) and not got[2][:5].any() and not got[2][13:].any()
+    inside = api.wpsgd_preference_loss(z, labels.cuda(), offsets, ref_log=ref_log.cuda(), beta=k.beta, scale=k.scale, grad=z)
+    assert torch.equal(inside[2], got[2]) and torch.equal(inside[0], got[0]) and (room[:, :3] == 2).all() and (room[:, c + 3:] == 2).all()
+
+
+def test_more_pairs_than_one_launch_takes_and_empty_ones():
+    pairs = 70000
+    k = Case(ends_of(1, 2, 0, 1), 20, "f32", 7, weighted=False)
+    ends = torch.zeros(2 * pairs + 1, dtype=torch.int64)
+    ends[-4:] = torch.tensor(k.ends[1:])
+    loss, margin, grad = api.wpsgd_preference_loss(k.z, k.labels.cuda(), ends.cuda(), ref_log=k.ref.cuda(), beta=k.beta, scale=k.scale)
+    want = k.run()
+    assert torch.equal(loss[-2:], want[0]) and torch.equal(margin[-2:], want[1]) and torch.equal(grad, want[2])
+    assert (margin[:-2] == 0).all() and ((loss[:-2] - math.log(2)).abs() <= 2.0 ** -24).all()

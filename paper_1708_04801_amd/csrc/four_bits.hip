@@ -207,20 +207,20 @@ struct Matmul4Args {
 // Every other call.  The classes' codes go from memory straight into the matrix instructions, two blocks (a line of 128 bytes) of NT sixteens of classes at a time to a wave.  Row i of a
 // tile of sixteen rows is row 4 (i mod 4) + i / 4 of the instruction, so that up to four rows need one result register of a lane, up to eight two (R).  A group's products are summed by
 // themselves and times its scale added in fp32.  Of WAVES waves in a workgroup `along` share the sum, pairs of blocks in turn, and add up through LDS in their order; the others take the next
-// classes.  HELD: the rows lie in LDS as fragments, up to WAVES * 8 KiB of the sum at a time, fp32 ones as three parts; else each wave asks for its own part of them.
+// classes.  HELD: the rows lie in LDS as fragments, up to 128 KiB of the sum at a time, fp32 ones as three parts; else each wave asks for its own part of them.
 // 8 x 65536 x 4096 fp32 (LDS) 43 us, 3.2 TB/s of codes; 1 x 4096 x 4096 (each wave) 7.1, a launch and three trips to memory one behind the other (row number, row, sum);
-// 64 x 65536 x 4096 73, 470 TFLOP/s: fragments from LDS and codes widened for four tiles of rows at a time.
-template <int MT, int R, int PARTS, int WAVES> constexpr int held_blocks4()
+// 64 x 65536 x 4096 68, 500 TFLOP/s (74 with 64 KiB of rows at a time): fragments from LDS and codes widened for four tiles of rows at a time.
+template <int MT, int R, int PARTS> constexpr int held_blocks4()
 {
     int n = 64;
-    while (n > 2 && n * MT * R * PARTS > WAVES * 8) n /= 2;
+    while (n > 2 && n * MT * R * PARTS > 128) n /= 2;
     return n;
 }
 
 // pairs of blocks on their way while one is worked on
-template <int MT, int R, int NT, int PARTS, int WAVES> constexpr int ahead4()
+template <int MT, int R, int NT, int PARTS> constexpr int ahead4()
 {
-    const int pairs = held_blocks4<MT, R, PARTS, WAVES>() / 2, most = NT == 1 ? 4 : 2;
+    const int pairs = held_blocks4<MT, R, PARTS>() / 2, most = NT == 1 ? 4 : 2;
     return pairs < most ? pairs : most;
 }
 // a barrier for what lies in LDS: loads from memory stay on their way
@@ -229,8 +229,8 @@ __device__ inline void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_b
 template <typename T, int MT, int R, int NT, int G, int WAVES, bool HELD>
 __global__ __launch_bounds__(64 * WAVES) void matmul4_kernel(Matmul4Args g, int along)
 {
-    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, kHeld = held_blocks4<MT, R, PARTS, WAVES>(), kLanes = 16 * R, kThreads = 64 * WAVES;
-    constexpr int kAhead = ahead4<MT, R, NT, PARTS, WAVES>();
+    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, kHeld = held_blocks4<MT, R, PARTS>(), kLanes = 16 * R, kThreads = 64 * WAVES;
+    constexpr int kAhead = ahead4<MT, R, NT, PARTS>();
     constexpr int kSums = MT * NT * R;
     __shared__ union {
         bf16x8v held[HELD ? kHeld * MT * 4 * PARTS : 1][kLanes];
@@ -674,7 +674,7 @@ __global__ __launch_bounds__(64 * kStreamWaves) void matmul4_stream_kernel(Matmu
 template <typename T, int MT, int R, int NT, int G, int WAVES, bool HELD>
 static hipError_t launch_rows(Matmul4Args g, hipStream_t s)
 {
-    constexpr int kHeld = held_blocks4<MT, R, sizeof(T) == 4 ? 3 : 1, WAVES>(), kAhead = ahead4<MT, R, NT, sizeof(T) == 4 ? 3 : 1, WAVES>();
+    constexpr int kHeld = held_blocks4<MT, R, sizeof(T) == 4 ? 3 : 1>(), kAhead = ahead4<MT, R, NT, sizeof(T) == 4 ? 3 : 1>();
     const int64_t groups = (g.classes + 16 * NT - 1) / (16 * NT), panels = (g.n + 16 * MT - 1) / (16 * MT), pairs = (g.blocks + 1) / 2;
     int along = 1;
     while (along < WAVES && (!HELD || along * 2 * kAhead <= kHeld / 2) && along < pairs && groups * panels * along < 256 * WAVES) along *= 2;
@@ -709,8 +709,8 @@ static hipError_t launch_matmul4(const Matmul4Args &g, hipStream_t s)
     // More classes than a workgroup on every compute unit takes at a time, and rows that the waves' registers hold: the stream (bfloat16, us, stream | rows in LDS | rows asked for by each
     // wave: 1 x 65536 x 4096 28.3 | 34.0 | 45.5, 16 x 65536 x 4096 33.5 | 35.8 | 85.6, 4 x 16384 x 4096 11.5 | 15.6 | 14.9; 1 x 4096 x 4096, one tile a workgroup, 11.1 | 14.1 | 7.1).
     if (rows <= 16 && pairs <= 16 && tiles * along > 256 * 16) return rows <= 4 ? launch_stream<1, G>(g, along, s) : launch_stream<4, G>(g, along, s);
-    // Rows in LDS where many classes share them, else asked for by each wave (us, in LDS | by each wave: 64 x 65536 x 4096 74 | 175 bfloat16, 139 | 285 fp32; 256 x 16384 x 4096 66 | 170;
-    // 64 x 16384 x 4096 63 | 47, 127 | 77 fp32; 37 x 5003 x 3001 fp32 95 | 23; 20 x 20000 x 1000 fp32 23.3 | 24.0; 8 x 65536 x 4096 fp32 43 | 92).
+    // Rows in LDS where many classes share them, else asked for by each wave (us, in LDS | by each wave: 64 x 65536 x 4096 68 | 169 bfloat16, 143 | 286 fp32; 256 x 16384 x 4096 61 | 167;
+    // 64 x 16384 x 4096 44 | 46, 133 | 75 fp32; 37 x 5003 x 3001 fp32 92 | 18; 20 x 20000 x 1000 fp32 22.7 | 24.6; 8 x 65536 x 4096 fp32 43 | 92).
     if (g.n <= 16 ? tiles > 1024 : tiles * ((g.n + 63) / 64) >= 2048) {
         if (g.n <= 8) return launch_rows<T, 1, 2, 1, G, 16, true>(g, s);
         if (g.n <= 16) return launch_rows<T, 1, 4, 1, G, 16, true>(g, s);

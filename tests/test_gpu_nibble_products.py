@@ -8,7 +8,7 @@ pytestmark = pytest.mark.gpu
 
 # rows in registers (few rows, many classes), rows in LDS, rows asked for by each wave; whole blocks and rows that end inside one
 SHAPES = [(1, 65600, 512), (4, 20000, 4096), (5, 20000, 4093), (16, 33000, 1000), (3, 5000, 9000), (7, 20000, 300), (12, 17000, 2050), (20, 40000, 384), (50, 34000, 260), (130, 17000, 256),
-          (1, 64, 4096), (9, 700, 1111), (30, 3000, 640), (64, 1000, 200), (37, 5003, 301)]
+          (24, 33000, 2300), (70, 17000, 2305), (1, 64, 4096), (9, 700, 1111), (30, 3000, 640), (64, 1000, 200), (37, 5003, 301)]
 
 
 @pytest.mark.parametrize("group", [32, 64, 128])

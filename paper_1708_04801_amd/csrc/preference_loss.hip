@@ -78,7 +78,7 @@ __device__ inline double pair_result(const PairArgs &a, int64_t p, double h, dou
     double slope, back;
     double loss = pair_loss(h, a.hinge != 0, slope);
     if (a.smoothing != 0.0) {
-        loss = (1.0 - a.smoothing) * loss + a.smoothing * pair_loss(-h, a.hinge != 0, back);
+        loss = (a.smoothing != 1.0 ? (1.0 - a.smoothing) * loss : 0.0) + a.smoothing * pair_loss(-h, a.hinge != 0, back);   // (loss may be infinite)
         slope = (1.0 - a.smoothing) * slope - a.smoothing * back;
     }
     if (writes) {
@@ -88,10 +88,13 @@ __device__ inline double pair_result(const PairArgs &a, int64_t p, double h, dou
     return -a.scale * a.beta * w * slope;
 }
 
-// A workgroup a pair: 16 pairs of 512 rows 12.5 us with a wave to each, which asked for its rows' gains eight times one behind the other.
-__global__ __launch_bounds__(256) void pair_kernel(PairArgs a)
+// A workgroup a pair, four rows to a thread at a time, all asked for before the first is added (one pair of 131072 rows, with the passes over 1024 bfloat16 scores a row: 430 us with 256
+// threads that ask for one at a time, 213 so; 1024 pairs of 8 rows, of 4099 scores: 43 with 256 threads to a pair, 49 with 1024).
+constexpr int kPairRows = 4;
+template <int kPairThreads>
+__global__ __launch_bounds__(kPairThreads) void pair_kernel(PairArgs a)
 {
-    __shared__ double part[4];
+    __shared__ double part[kPairThreads / 64];
     const int64_t p = a.first + blockIdx.x;
     const int t = threadIdx.x;
     const int64_t from = a.offsets[2 * p], middle = a.offsets[2 * p + 1], to = a.offsets[2 * p + 2];
@@ -101,15 +104,35 @@ __global__ __launch_bounds__(256) void pair_kernel(PairArgs a)
         return;
     }
     double sum = 0.0;
-    for (int64_t i = from + t; i < to; i += 256) sum += i < middle ? a.rows.gain[i] : -a.rows.gain[i];
+    for (int64_t i = from + t; i < to; i += kPairThreads * kPairRows) {
+        double gain[kPairRows];
+#pragma unroll
+        for (int y = 0; y < kPairRows; ++y) gain[y] = i + y * kPairThreads < to ? a.rows.gain[i + y * kPairThreads] : 0.0;
+#pragma unroll
+        for (int y = 0; y < kPairRows; ++y) sum += i + y * kPairThreads < middle ? gain[y] : -gain[y];
+    }
     sum = wave_sum(sum);
     if ((t & 63) == 0) part[t >> 6] = sum;
     __syncthreads();
-    const double f = pair_result(a, p, a.beta * (((part[0] + part[1]) + part[2]) + part[3]), w, t == 0);
+    sum = part[0];
+#pragma unroll
+    for (int o = 1; o < kPairThreads / 64; ++o) sum += part[o];
+    const double f = pair_result(a, p, a.beta * sum, w, t == 0);
     if (w == 0.0) return;
-    for (int64_t i = from + t; i < to; i += 256) {
-        const double r = a.row_weights ? (double)a.row_weights[i] : 1.0;
-        if (a.labels[i] >= 0 && r != 0.0) a.rows.factor[i] = (float)(i < middle ? f * r : -f * r);
+    for (int64_t i = from + t; i < to; i += kPairThreads * kPairRows) {
+        int64_t label[kPairRows];
+        float r[kPairRows];
+#pragma unroll
+        for (int y = 0; y < kPairRows; ++y) {
+            const int64_t row = i + y * kPairThreads;
+            label[y] = row < to ? a.labels[row] : -1;
+            r[y] = row < to && a.row_weights ? a.row_weights[row] : 1.0f;
+        }
+#pragma unroll
+        for (int y = 0; y < kPairRows; ++y) {
+            const int64_t row = i + y * kPairThreads;
+            if (label[y] >= 0 && r[y] != 0.0f) a.rows.factor[row] = (float)(row < middle ? f * (double)r[y] : -f * (double)r[y]);
+        }
     }
 }
 
@@ -293,9 +316,10 @@ static hipError_t launch_preference(RowArgs a, const GainOfRow &op, PairArgs p, 
     }
     hipError_t e = launch_rows_softmax<T>(a, op, s);
     if (e == hipSuccess)
-        e = in_launches(p.pairs, 256, [&](int64_t first, unsigned count) {
+        e = in_launches(p.pairs, 1024, [&](int64_t first, unsigned count) {
             p.first = first;
-            hipLaunchKernelGGL(pair_kernel, dim3(count), dim3(256), 0, s, p);
+            if (p.n <= 256 * p.pairs) hipLaunchKernelGGL(pair_kernel<256>, dim3(count), dim3(256), 0, s, p);
+            else hipLaunchKernelGGL(pair_kernel<1024>, dim3(count), dim3(1024), 0, s, p);
         });
     if (e != hipSuccess || !grad) return e;
     a.grad = grad;

@@ -103,7 +103,7 @@ def test_results_for_a_named_stream_are_not_memory_that_the_current_one_still_wr
     assert same(want, result(out))
 
 
-def test_the_whole_rounds_gradients_match_differences():
+def test_gradients_of_scores_through_all_of_them_match_differences():
     """the class vectors' gradient of the policy loss, through scores in 8-bit blocks, against differences of the loss along it: a step of h against the gradient lowers the
     loss by h times its squared norm"""
     n, classes, d = 64, 200, 256

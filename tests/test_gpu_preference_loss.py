@@ -242,3 +242,39 @@ def test_more_pairs_than_one_launch_takes_and_empty_ones():
     want = k.run()
     assert torch.equal(loss[-2:], want[0]) and torch.equal(margin[-2:], want[1]) and torch.equal(grad, want[2])
     assert (margin[:-2] == 0).all() and ((loss[:-2] - math.log(2)).abs() <= 2.0 ** -24).all()
+
+
+@pytest.mark.parametrize("kind", [api.HINGE, api.LOGISTIC])
+@pytest.mark.parametrize("c,dtype", [(20, "f32"), (3000, "bf16")])
+def test_a_margin_without_end_and_whole_smoothing(c, dtype, kind):
+    """smoothing 1 is the loss of the other sequence's preference, also where the margin is infinite: nothing is left of L(h)"""
+    z = torch.randn(3, c, generator=torch.Generator().manual_seed(5)).to(DTYPES[dtype])
+    z[0, 1] = -math.inf
+    loss, margin, grad = api.wpsgd_preference_loss(z.cuda(), torch.tensor([1, 0, 0]).cuda(), torch.tensor([0, 1, 3]).cuda(), kind=kind, smoothing=1.0)
+    assert margin.item() == -math.inf and loss.item() == 0 and not grad.any()
+    loss, margin, grad = api.wpsgd_preference_loss(z.cuda(), torch.tensor([1, 0, 0]).cuda(), torch.tensor([0, 1, 3]).cuda(), kind=kind, smoothing=0.5)
+    assert margin.item() == -math.inf and loss.item() == math.inf
+
+
+@pytest.mark.parametrize("lengths", [(3000, 2500), (5000, 0), (1, 9000)])
+def test_long_sequences(lengths):
+    """more rows than a workgroup takes at once in one pair: the margin is the sum of what each row comes to by itself, and the gradient goes by that margin"""
+    n, c = sum(lengths), 6
+    k = Case(ends_of(*lengths), c, "f32", 8)
+    k.labels[::7] = -1
+    loss, margin, grad = (t.double().cpu() for t in k.run())
+    alone = api.wpsgd_preference_loss(k.z, k.labels.cuda(), torch.arange(2 * n + 1).div(2, rounding_mode="floor").add(torch.arange(2 * n + 1) % 2).cuda(), ref_log=k.ref.cuda(),
+                                      row_weights=k.w.float().cuda(), beta=k.beta, grad=False)[1].double().cpu()
+    sign = torch.where(torch.arange(n) < lengths[0], 1.0, -1.0).double()
+    # each row's margin is rounded once, and the whole once
+    h = (sign * alone).sum()
+    assert (margin - h).abs() <= 2.0 ** -24 * (alone.abs().sum() + h.abs()) + 1e-12 * alone.abs().sum()
+    w = k.pw.double()
+    assert (loss - w * torch.nn.functional.softplus(-h)).abs() <= w * (margin - h).abs() + 2.0 ** -24 * loss + 2.0 ** -24 * w * alone.abs().sum()
+    f = -k.scale * k.beta * w * torch.sigmoid(-h) * k.w.double() * sign * (k.labels >= 0)
+    p = torch.softmax(k.z.double().cpu(), 1)
+    hot = torch.zeros(n, c, dtype=torch.float64)
+    hot[torch.arange(n), k.labels.clamp(min=0)] = 1
+    # d loss / d z = f (hot - p); the slope moves by no more than the margin does, of itself
+    off = 2.0 ** -24 * alone.abs().sum() + 2.0 ** -22
+    assert ((grad - f[:, None] * (hot - p)).abs() <= f.abs()[:, None] * (DELTA * p + off * (hot + p)) + 1e-37).all() and not grad[::7].any()

@@ -182,14 +182,16 @@ __global__ __launch_bounds__(256) void pair_gradient_kernel(RowArgs a, RowResult
     }
 }
 
-// Short rows and few of them: a workgroup forms a whole pair, its waves a row each in turn, statistics first and, when the pair's margin is known, once more with the gradient; the rows
-// come out of the caches then.  One launch instead of three: 6 pairs of 18 rows of 1001 fp32 scores, 12.9 instead of 19.1 us a call, of which the host takes most.  The workgroups behind the pairs' zero the gradient of rows that no sequence holds.
+// Short rows and few of them: a workgroup forms a whole pair, its waves a row each in turn, statistics first (and for all its rows at once what a lane makes of each) and, when the pair's
+// margin is known, the gradient, of the last row out of the registers, of the others once more from the caches.  One launch instead of three: 6 pairs of 18 rows of 1001 fp32 scores, 11.3 us
+// a call of which the host takes most.  The workgroups behind the pairs' zero the gradient of rows that no sequence holds.
 constexpr int kPairWaves = 16, kPairVectors = 4;
 template <typename T> constexpr int64_t most_pair_classes() { return 64 * kPairVectors * Elem<T>::kPer16; }
 static bool pair_in_one(int64_t n, int64_t classes, int64_t pairs, wpsgd_dtype dtype)
 {
-    // (all rows may belong to one pair: its workgroup then passes over 64 rows a wave, some 80 us)
-    return classes <= (dtype == WPSGD_F32 ? most_pair_classes<float>() : most_pair_classes<uint16_t>()) && n <= 1024 && n <= 64 * pairs && pairs <= 65536;
+    // us a call, so | by three kernels (these in a graph 10): 32 rows of one pair 12.3 | 18.4 (1001 fp32), 14.0 | 18.5 (2000 bfloat16); 64 of one 20 | 18.4; 200 of three 21 | 18.4.
+    // All rows may belong to one pair: 256 take some 70.
+    return classes <= (dtype == WPSGD_F32 ? most_pair_classes<float>() : most_pair_classes<uint16_t>()) && n <= 256 && n <= 32 * pairs && pairs <= 65536;
 }
 
 template <typename T>
@@ -218,50 +220,72 @@ __global__ __launch_bounds__(64 * kPairWaves) void whole_pair_kernel(PairArgs a,
         if (threadIdx.x == 0) a.loss[p] = a.margin[p] = __builtin_nanf("");
         return;
     }
-    // a row's scores become exponentials relative to its maximum
-    float x[V * E], last, m;
-    double s;
-    auto row_of = [&](int64_t row) {
-        const T *q = static_cast<const T *>(z.z) + row * z.ld;
-        Bytes16 raw[V];
+    // Row wave + 16 i of the pair is the wave's i-th, and lane i keeps what is known of it.
+    const int count = to - from > wave ? (int)((to - from - wave + kPairWaves - 1) / kPairWaves) : 0;
+    const int64_t row0 = from + wave, mine = row0 + (int64_t)lane * kPairWaves;
+    Bytes16 raw[V];
+    float last;
+    auto ask = [&](int i) {
+        const T *q = static_cast<const T *>(z.z) + (row0 + (int64_t)i * kPairWaves) * z.ld;
 #pragma unroll
         for (int v = 0; v < V; ++v) raw[v] = v * 64 + lane < vectors ? load16(q + (int64_t)(v * 64 + lane) * E) : Bytes16{{0, 0, 0, 0}};
         last = lane < tail ? Elem<T>::load(q + (int64_t)vectors * E + lane) : -kInf;
-        m = last;
+    };
+    if (count) ask(0);                                                            // (before it is known whether it counts)
+    const int64_t label = lane < count ? z.labels[mine] : -1;
+    const float r = lane < count && z.row_weights ? z.row_weights[mine] : 1.0f;
+    const double ref = lane < count && ref_log ? (double)ref_log[mine] : 0.0;
+    const bool counts = label >= 0 && r != 0.0f;
+    const uint64_t all = __ballot(counts), none = __ballot(lane < count && !counts);
+    const float z_label = counts && label < z.c ? Elem<T>::load(static_cast<const T *>(z.z) + mine * z.ld + label) : 0.0f;
+    // the scores asked for become exponentials relative to the row's maximum m
+    float x[V * E], x_last = 0.0f, m = -kInf, my_m = -kInf;
+    double my_s = 0.0;
+    auto take = [&]() {
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
-            for (int j = 0; j < E; ++j) {
-                x[v * E + j] = v * 64 + lane < vectors ? Elem<T>::get(raw[v].w, j) : -kInf;
-                m = fmaxf(m, x[v * E + j]);
-            }
-        m = wave_max(fmaxf(m, -kInf));
+            for (int j = 0; j < E; ++j) x[v * E + j] = v * 64 + lane < vectors ? Elem<T>::get(raw[v].w, j) : -kInf;
+        x_last = last;
+    };
+    auto exponentials = [&]() {
         const float base = m == -kInf ? 0.0f : m;
-        last = exp_for<T, true>(last - base);
-        s = last;
+        x_last = exp_for<T, true>(x_last - base);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
+            if (v * 64 >= vectors) break;
+#pragma unroll
+            for (int j = v * E; j < v * E + E; ++j) x[j] = exp_for<T, true>(x[j] - base);
+        }
+    };
+    int held = -1;                                                                // the row whose exponentials the registers hold
+    for (uint64_t left = all; left; left &= left - 1) {
+        const int i = __builtin_ctzll(left), next = (left & (left - 1)) ? __builtin_ctzll(left & (left - 1)) : i;
+        if (held < 0 && i != 0) ask(i);
+        take();
+        ask(next);
+        m = x_last;
+#pragma unroll
+        for (int j = 0; j < V * E; ++j) m = fmaxf(m, x[j]);
+        m = wave_max(fmaxf(m, -kInf));
+        exponentials();
+        double s = x_last;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            if (v * 64 >= vectors) break;
             float eight = 0.0f;
 #pragma unroll
-            for (int j = v * E; j < v * E + E; ++j) {
-                x[j] = exp_for<T, true>(x[j] - base);
-                eight += x[j];
-            }
+            for (int j = v * E; j < v * E + E; ++j) eight += x[j];
             s += eight;
         }
         s = wave_sum(s);
-    };
-    double sum = 0.0;
-    for (int64_t row = from + wave; row < to; row += kPairWaves) {
-        const int64_t label = z.labels[row];
-        const float r = z.row_weights ? z.row_weights[row] : 1.0f;
-        if (label < 0 || r == 0.0f) continue;
-        const float z_label = label < z.c ? Elem<T>::load(static_cast<const T *>(z.z) + row * z.ld + label) : 0.0f;
-        const double ref = ref_log ? (double)ref_log[row] : 0.0;
-        row_of(row);
-        const double gain = gain_of(RowState{m, (float)s, z_label, s, m == -kInf && s == 0.0, label >= z.c}, r, ref);
-        sum += row < middle ? gain : -gain;
+        my_m = lane == i ? m : my_m;
+        my_s = lane == i ? s : my_s;
+        held = i;
     }
+    const bool empty = my_m == -kInf && my_s == 0.0;                              // no class left
+    double sum = counts ? gain_of(RowState{my_m, (float)my_s, z_label, my_s, empty, label >= z.c}, r, ref) : 0.0;
+    sum = wave_sum(mine < middle ? sum : -sum);
     if (lane == 0) part[wave] = sum;
     __syncthreads();                                                              // (every row's scores have been read: the gradient may take their place)
     sum = part[0];
@@ -269,22 +293,27 @@ __global__ __launch_bounds__(64 * kPairWaves) void whole_pair_kernel(PairArgs a,
     for (int o = 1; o < kPairWaves; ++o) sum += part[o];
     const double f0 = pair_result(a, p, a.beta * sum, w, threadIdx.x == 0);
     if (!z.grad) return;
-    for (int64_t row = from + wave; row < to; row += kPairWaves) {
-        const int64_t label = z.labels[row];
-        const float r = z.row_weights ? z.row_weights[row] : 1.0f;
-        const float f = (float)(row < middle ? f0 * (double)r : -f0 * (double)r);
-        if (label < 0 || r == 0.0f || w == 0.0 || f == 0.0f) {
-            zero(row);
-            continue;
+    const float f = (float)(mine < middle ? f0 * (double)r : -f0 * (double)r), over = f / (float)my_s;
+    const int at_label = label < z.c ? (int)label : -1;
+    const uint64_t nothing = none | __ballot(counts && (w == 0.0 || f == 0.0f || empty));
+    for (uint64_t left = nothing; left; left &= left - 1) zero(row0 + (int64_t)__builtin_ctzll(left) * kPairWaves);
+    // from the last row on, which is there
+    uint64_t left = all & ~nothing;
+    int next = left ? 63 - __builtin_clzll(left) : 0;
+    if (left && next != held) ask(next);
+    while (left) {
+        const int i = next;
+        left &= ~(1ull << i);
+        next = left ? 63 - __builtin_clzll(left) : i;
+        if (i != held) take();
+        if (left) ask(next);
+        if (i != held) {
+            m = __shfl(my_m, i);
+            exponentials();
         }
-        row_of(row);
-        if (m == -kInf && s == 0.0) {                                            // no class left
-            zero(row);
-            continue;
-        }
-        T *g = static_cast<T *>(z.grad) + row * z.ld_grad;
-        const float over = f / (float)s;
-        const int at_label = label < z.c ? (int)label : -1;
+        const float f_i = __shfl(f, i), over_i = __shfl(over, i);
+        const int at_i = __shfl(at_label, i);
+        T *g = static_cast<T *>(z.grad) + (row0 + (int64_t)i * kPairWaves) * z.ld_grad;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             if (v * 64 + lane >= vectors) continue;
@@ -292,14 +321,14 @@ __global__ __launch_bounds__(64 * kPairWaves) void whole_pair_kernel(PairArgs a,
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int at = (v * 64 + lane) * E + j * E / 4;
-                if constexpr (E == 8) o.w[j] = bf16_pack(x[v * E + 2 * j] * over - (at == at_label ? f : 0.0f), x[v * E + 2 * j + 1] * over - (at + 1 == at_label ? f : 0.0f));
-                else o.w[j] = __float_as_uint(x[v * E + j] * over - (at == at_label ? f : 0.0f));
+                if constexpr (E == 8) o.w[j] = bf16_pack(x[v * E + 2 * j] * over_i - (at == at_i ? f_i : 0.0f), x[v * E + 2 * j + 1] * over_i - (at + 1 == at_i ? f_i : 0.0f));
+                else o.w[j] = __float_as_uint(x[v * E + j] * over_i - (at == at_i ? f_i : 0.0f));
             }
             store16(g + (int64_t)(v * 64 + lane) * E, o);
         }
         if (lane < tail) {
             const int at = vectors * E + lane;
-            Elem<T>::put(g + at, last * over - (at == at_label ? f : 0.0f));
+            Elem<T>::put(g + at, x_last * over_i - (at == at_i ? f_i : 0.0f));
         }
     }
 }

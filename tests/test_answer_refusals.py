@@ -45,10 +45,10 @@ def test_preference_workspace():
     need = L.wpsgd_preference_loss_workspace(1000, 3000, 20, api.F32)
     assert need >= 20000 and need % 256 == 0
     assert preference(n=1000, pairs=20, ws_bytes=need - 1) == api.WORKSPACE_TOO_SMALL
-    # none for pairs that a workgroup forms by itself: up to 1024 classes in fp32, 2048 in bfloat16, 1024 rows, 64 rows a pair on average
+    # none for pairs that a workgroup forms by itself: up to 1024 classes in fp32, 2048 in bfloat16, 256 rows, 32 rows a pair on average
     one = lambda n, c, pairs, dtype: L.wpsgd_preference_loss_workspace(n, c, pairs, dtype) == 0  # noqa: E731
-    assert one(0, 3000, 1, api.F32) and one(-1, 3000, 1, api.F32) and one(1024, 1024, 16, api.F32) and one(1024, 2048, 16, api.BF16) and one(64, 1, 1, api.F32)
-    assert not (one(1024, 1025, 16, api.F32) or one(1024, 2049, 16, api.BF16) or one(1025, 1024, 17, api.F32) or one(1024, 1024, 15, api.F32) or one(1, 8, 0, api.F32))
+    assert one(0, 3000, 1, api.F32) and one(-1, 3000, 1, api.F32) and one(256, 1024, 8, api.F32) and one(256, 2048, 8, api.BF16) and one(32, 1, 1, api.F32)
+    assert not (one(256, 1025, 8, api.F32) or one(256, 2049, 8, api.BF16) or one(257, 1024, 17, api.F32) or one(256, 1024, 7, api.F32) or one(1, 8, 0, api.F32))
     assert preference(n=0, pairs=0, Z=None, labels=None, loss=None, margin=None, ws=None) == api.OK
 
 

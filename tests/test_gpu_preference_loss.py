@@ -278,3 +278,32 @@ def test_long_sequences(lengths):
     # d loss / d z = f (hot - p); the slope moves by no more than the margin does, of itself
     off = 2.0 ** -24 * alone.abs().sum() + 2.0 ** -22
     assert ((grad - f[:, None] * (hot - p)).abs() <= f.abs()[:, None] * (DELTA * p + off * (hot + p)) + 1e-37).all() and not grad[::7].any()
+
+
+@pytest.mark.parametrize("lengths,c", [((17, 15), 1023), ((100, 90, 1, 1) + (1, 0) * 6, 300), ((0, 240) + (1, 1) * 7, 65), ((33, 31, 16, 16, 0, 0, 1, 2), 1024)])
+def test_both_ways_to_form_a_pair_agree(lengths, c):
+    """up to 256 rows in a launch, and the same with as many behind them that it takes three: the same exponentials in fp64 sums of another order, rounded once"""
+    k = Case(ends_of(*lengths), c, "f32", 21)
+    n = k.n
+    k.labels[::5] = -1
+    k.w[3] = 0.0
+    k.z[0] = math.nan
+    k.z[7, : c // 2] = -math.inf
+    one = k.run()
+    z = torch.cat([k.z, torch.zeros(300, c, device="cuda")])
+    grow = lambda t, value: torch.cat([t, torch.full((300,), value, dtype=t.dtype)]).cuda()  # noqa: E731
+    for inside in (False, True):
+        x = z.clone()
+        loss, margin, grad = api.wpsgd_preference_loss(x, grow(k.labels, 0), torch.tensor(k.ends).cuda(), ref_log=grow(k.ref, 0.0), row_weights=grow(k.w.float(), 1.0),
+                                                       pair_weights=k.pw.float().cuda(), beta=k.beta, scale=k.scale, grad=x if inside else True)
+        far = margin.abs().nan_to_num(0.0, 0.0)
+        near = lambda a, b, off: ((a == b) | ((a - b).abs() <= off)).all()  # noqa: E731    (equal infinities are equal)
+        assert near(loss, one[0], 2.0 ** -23 * (loss.abs() + far * k.pw.float().cuda())) and near(margin, one[1], 2.0 ** -23 * far)
+        # f p - f [label]: a factor that moves with the margin, its quotient by the sum, two roundings of either side
+        size = abs(k.scale * k.beta) * float(k.w.max() * k.pw.max()) * 2.0 ** -21 * (1 + float(far.max()))
+        assert near(grad[:n], one[2], 2.0 ** -20 * (1 + far.max()) * grad[:n].abs() + size * (grad[:n] != 0)) and not grad[n:].any()
+        assert not grad[:n][torch.arange(0, n, 5)].any() and not grad[3].any()
+    k.z[0] = 0.0                                  # (the oracle reads it)
+    k.check(k.run())
+    keep = k.run(grad=k.z)
+    assert torch.equal(keep[0], one[0]) and torch.equal(keep[2], one[2])

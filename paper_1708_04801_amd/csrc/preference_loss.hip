@@ -28,10 +28,8 @@ struct GainOfRow {
     static constexpr bool kOneWave = true, kWideSum = true;
     RowResult to;
     const float *ref_log;
-    const int64_t *ends;       // where the first sequence begins
-    int64_t sequences;
-    // (what no sequence holds is not looked at)
-    __device__ bool counts(int64_t row, int64_t label, float r) const { return !(label < 0 || r == 0.0f) && row >= ends[0] && row < ends[sequences]; }
+    // (rows that no sequence holds too: no pair adds them up, and their factors stay 0.  The first and the last offset could tell them apart only if all offsets were right.)
+    __device__ bool counts(int64_t, int64_t label, float r) const { return !(label < 0 || r == 0.0f); }
     __device__ void absent(int64_t row) const
     {
         to.factor[row] = 0.0f;
@@ -387,7 +385,7 @@ int wpsgd_preference_loss(const void *Z, int64_t n, int64_t classes, int64_t ld,
     const RowResult to{reinterpret_cast<float2 *>(static_cast<double *>(workspace) + n), reinterpret_cast<float *>(static_cast<double *>(workspace) + 2 * n),
                        static_cast<double *>(workspace)};
     const RowArgs a{Z, n, classes, ld, labels, row_weights, nullptr, ld_grad, 0};
-    const GainOfRow op{to, ref_log, offsets, 2 * pairs};
+    const GainOfRow op{to, ref_log};
     const PairArgs p{labels, offsets, n, pairs, row_weights, pair_weights, kind == WPSGD_HINGE, beta, smoothing, scale, to, loss, margin, 0};
     const bool in_one = pair_in_one(n, classes, pairs, dtype);
     hipStream_t s = static_cast<hipStream_t>(stream);

@@ -441,7 +441,7 @@ int wpsgd_policy_loss(const void *Z, int64_t n, int64_t classes, int64_t ld, wps
  * both are -inf.  A label >= classes makes the pair's results NaN, and so does a score of a row that counts which is +inf or NaN.
  *   Z             DEVICE, n x classes, row stride ld elements, fp32 or bfloat16    labels  DEVICE, n
  *   offsets       DEVICE, 2 * pairs + 1 row numbers, none under the one before it, within 0 .. n.  Where a pair's three are not, its loss and margin are NaN, the
- *                 other pairs' are what they are without it, and nothing is said about the gradient.  (Rows that no sequence holds are read all the same, unless
+ *                 other pairs' are what they are without it, and nothing is said about the gradient (in place Z may hold the scores still).  (Rows that no sequence holds are read all the same, unless
  *                 their labels are negative.)
  *   ref_log       DEVICE, n fp32 (-loss of wpsgd_softmax_loss under a reference), or NULL for zeros
  *   row_weights   DEVICE, n fp32 (r_i), or NULL for ones         pair_weights  DEVICE, pairs fp32 (w_p), or NULL for ones

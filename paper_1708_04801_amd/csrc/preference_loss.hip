@@ -183,13 +183,13 @@ __global__ __launch_bounds__(256) void pair_gradient_kernel(RowArgs a, RowResult
 // Short rows and few of them: a workgroup forms a whole pair, its waves a row each in turn, statistics first (and for all its rows at once what a lane makes of each) and, when the pair's
 // margin is known, the gradient, of the last row out of the registers, of the others once more from the caches.  One launch instead of three: 6 pairs of 18 rows of 1001 fp32 scores, 11.3 us
 // a call of which the host takes most.  The workgroups behind the pairs' zero the gradient of rows that no sequence holds.
-constexpr int kPairWaves = 16, kPairVectors = 4;
+constexpr int kPairWaves = 16, kPairVectors = 4, kMostPairs = 32 * kPairWaves;      // (a thread looks at one step between two offsets)
 template <typename T> constexpr int64_t most_pair_classes() { return 64 * kPairVectors * Elem<T>::kPer16; }
 static bool pair_in_one(int64_t n, int64_t classes, int64_t pairs, wpsgd_dtype dtype)
 {
     // us a call, so | by three kernels (these in a graph 10): 32 rows of one pair 12.3 | 18.4 (1001 fp32), 14.0 | 18.5 (2000 bfloat16); 64 of one 20 | 18.4; 200 of three 21 | 18.4.
-    // All rows may belong to one pair: 256 take some 70.
-    return classes <= (dtype == WPSGD_F32 ? most_pair_classes<float>() : most_pair_classes<uint16_t>()) && n <= 256 && n <= 32 * pairs && pairs <= 65536;
+    // All rows may belong to one pair: 256 take some 70.  Pairs of a row or none (200 rows of 300 fp32, in a graph): 300 pairs 8.5, 513 of them 10.6 | 10.0, 1000 15.4 | 10.7, 4000 48 | 15.
+    return classes <= (dtype == WPSGD_F32 ? most_pair_classes<float>() : most_pair_classes<uint16_t>()) && n <= 256 && n <= 32 * pairs && pairs <= kMostPairs;
 }
 
 template <typename T>
@@ -198,6 +198,7 @@ __global__ __launch_bounds__(64 * kPairWaves) void whole_pair_kernel(PairArgs a,
     constexpr int E = Elem<T>::kPer16, V = kPairVectors;
     constexpr float kInf = __builtin_inff();
     __shared__ double part[kPairWaves];
+    __shared__ bool falls[kPairWaves];
     const int64_t p = blockIdx.x;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (int)z.c, vectors = c / E, tail = c - vectors * E;
     auto zero = [&](int64_t row) {
@@ -205,8 +206,12 @@ __global__ __launch_bounds__(64 * kPairWaves) void whole_pair_kernel(PairArgs a,
         for (int v = lane; v < vectors; v += 64) store16(g + (int64_t)v * E, Bytes16{{0, 0, 0, 0}});
         if (lane < tail) Elem<T>::put(g + (int64_t)vectors * E + lane, 0.0f);
     };
+    // A gradient that takes the scores' place: where an offset is under the one before it, a row may belong to two pairs, or to one and to none, and would be written before all have
+    // read it.  No gradient is written then.
+    const bool in_place = z.grad == z.z;
+    const bool down = in_place && threadIdx.x < 2 * a.pairs && a.offsets[threadIdx.x] > a.offsets[threadIdx.x + 1];
     if (p >= a.pairs) {
-        if (!z.grad) return;
+        if (!z.grad || (in_place && __syncthreads_or(down))) return;
         const int64_t first = a.offsets[0], last = a.offsets[2 * a.pairs], others = gridDim.x - a.pairs;
         for (int64_t row = (p - a.pairs) * kPairWaves + wave; row < a.n; row += others * kPairWaves)
             if (row < first || row >= last) zero(row);
@@ -284,13 +289,23 @@ __global__ __launch_bounds__(64 * kPairWaves) void whole_pair_kernel(PairArgs a,
     const bool empty = my_m == -kInf && my_s == 0.0;                              // no class left
     double sum = counts ? gain_of(RowState{my_m, (float)my_s, z_label, my_s, empty, label >= z.c}, r, ref) : 0.0;
     sum = wave_sum(mine < middle ? sum : -sum);
-    if (lane == 0) part[wave] = sum;
+    const bool wave_falls = __ballot(down) != 0;
+    if (lane == 0) {
+        part[wave] = sum;
+        falls[wave] = wave_falls;
+    }
     __syncthreads();                                                              // (every row's scores have been read: the gradient may take their place)
     sum = part[0];
 #pragma unroll
     for (int o = 1; o < kPairWaves; ++o) sum += part[o];
     const double f0 = pair_result(a, p, a.beta * sum, w, threadIdx.x == 0);
     if (!z.grad) return;
+    if (in_place) {
+        bool any = false;
+#pragma unroll
+        for (int o = 0; o < kPairWaves; ++o) any |= falls[o];
+        if (any) return;
+    }
     const float f = (float)(mine < middle ? f0 * (double)r : -f0 * (double)r), over = f / (float)my_s;
     const int at_label = label < z.c ? (int)label : -1;
     const uint64_t nothing = none | __ballot(counts && (w == 0.0 || f == 0.0f || empty));

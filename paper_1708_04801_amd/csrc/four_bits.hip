@@ -123,7 +123,7 @@ __device__ inline bf16x8v widen_codes(uint32_t w)
 }
 
 // Values as bfloat16 (PARTS 1: they are), or as sums of three bfloat16 values, eight significant bits each: what a value's upper half stands for, the same of the rest, and the rest of that.
-// What is not finite stays in the first.
+// What is not finite stays in the first; a NaN becomes the quiet one, since the bits that tell another from an infinity may all lie in the lower half.
 template <int PARTS>
 __device__ inline void split8(const float (&x)[8], bf16x8v *part)
 {
@@ -143,11 +143,14 @@ __device__ inline void split8(const float (&x)[8], bf16x8v *part)
             most += fabsf(rest[j]);                                                     // NaN where one is not finite
         }
         if (most != most) {
+            float whole[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
+                whole[j] = x[j] == x[j] ? x[j] : __builtin_nanf("");
                 last[j] = rest[j] == rest[j] ? last[j] : 0.0f;
                 rest[j] = rest[j] == rest[j] ? rest[j] : 0.0f;
             }
+            part[0] = halves(whole);
         }
         part[1] = halves(rest);
         part[2] = halves(last);

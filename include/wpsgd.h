@@ -489,7 +489,8 @@ typedef struct wpsgd_nibbles {
 int wpsgd_quantize_nibbles(const wpsgd_matrix *X, const int64_t *rows, int64_t n, const wpsgd_nibbles *out, void *stream);
 
 /* out[i*ld_out + j] = sum_c x(i, c) * W(j, c) for n rows of X (dense; CSR: UNSUPPORTED) and all rows j of W, made for few rows: every 64 of them read W once.  The values
- * of x are taken as they are (fp32 ones too), sums are fp32, rounded once to dtype; parts of fp32 elements under 2^-126 may be lost.
+ * of x are taken as they are (fp32 ones too), sums are fp32, rounded once to dtype.  A result that dtype holds comes out whatever the sizes of the elements; parts of fp32
+ * elements under 2^-126, and less than 2^-116 of a group's sum of elements times codes and of a result, may be lost.
  *   rows   as for wpsgd_quantize       out   DEVICE, n x W->rows; it may not overlap X or W
  * The result does not depend on timing.  Errors: INVALID_ARG, UNSUPPORTED (CSR), HIP_ERROR. */
 int wpsgd_nibble_matmul(const wpsgd_matrix *X, const int64_t *rows, int64_t n, const wpsgd_nibbles *W, void *out, int64_t ld_out, wpsgd_dtype dtype,

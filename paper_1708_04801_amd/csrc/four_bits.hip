@@ -114,11 +114,13 @@ typedef __bf16 bf16x8v __attribute__((ext_vector_type(8)));
 typedef float f32x4v __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
 
-// the eight values of a word's codes, as they are
+// The eight values of a word's codes, times 2^-10: a group's sum, which meets its scale only when it is whole, is under 2^128 then whatever the rows (6 * 128 < 2^10), and results that fp32
+// holds come out.  Results are multiplied by 2^10 where they are stored; both are exact, but for what that puts under 2^-126: less than 2^-116 of a group's sum or of a result.
+constexpr float kCodeScale = 0x1p-10f, kResultScale = 0x1p10f;
 __device__ inline bf16x8v widen_codes(uint32_t w)
 {
-    const bf16x2v a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 1),
-                  c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, 3);
+    const bf16x2v a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, kCodeScale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, kCodeScale, 1),
+                  c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, kCodeScale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, kCodeScale, 3);
     return bf16x8v{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
 }
 
@@ -500,6 +502,7 @@ __global__ __launch_bounds__(64 * WAVES) void matmul4_kernel(Matmul4Args g, int 
         if (c >= g.classes || h >= g.n) continue;
         float sum = lds.sums[w * along][v][l];
         for (int o = 1; o < along; ++o) sum += lds.sums[w * along + o][v][l];
+        sum *= kResultScale;
         if (g.half) Elem<uint16_t>::put(static_cast<uint16_t *>(g.out) + h * g.ld_out + c, sum);
         else Elem<float>::put(static_cast<float *>(g.out) + h * g.ld_out + c, sum);
     }
@@ -668,6 +671,7 @@ __global__ __launch_bounds__(64 * kStreamWaves) void matmul4_stream_kernel(Matmu
 #pragma unroll
                 for (int a = 0; a < kStreamWaves; ++a) sum += a < along ? one[a] : 0.0f;
             }
+            sum *= kResultScale;
             if (g.half) Elem<uint16_t>::put(static_cast<uint16_t *>(g.out) + h * g.ld_out + cls, sum);
             else Elem<float>::put(static_cast<float *>(g.out) + h * g.ld_out + cls, sum);
         }

@@ -425,8 +425,8 @@ int wpsgd_draw_classes(const void *Z, int64_t n, int64_t classes, int64_t ld, wp
  *   advantage  DEVICE, n         row_weights  DEVICE, n (r_i), or NULL for ones
  *   loss       DEVICE out, n     log_prob     DEVICE out, n, or NULL
  *   grad       DEVICE out, dtype as Z, row stride ld_grad; NULL: not wanted.  It may be Z itself (with ld_grad = ld), else it may not overlap it.
- * (All of them fp32 but Z, drawn and grad.)  -loss of wpsgd_softmax_loss without a gradient is a log probability too.  Exponentials are fp32, their sums and what a row makes
- * of them fp64; the result does not depend on timing.  Errors: INVALID_ARG (0 <= clip_low <= 1; clip_high >= 0, it may be infinite; kl >= 0), HIP_ERROR. */
+ * (All of them fp32 but Z, drawn and grad.)  -loss of wpsgd_softmax_loss without a gradient is a log probability too.  Exponentials are fp32, sums of more than eight of them and
+ * what a row makes of those fp64; the result does not depend on timing.  Errors: INVALID_ARG (0 <= clip_low <= 1; clip_high >= 0, it may be infinite; kl >= 0), HIP_ERROR. */
 int wpsgd_policy_loss(const void *Z, int64_t n, int64_t classes, int64_t ld, wpsgd_dtype dtype, const int64_t *drawn, const float *old_log,
                       const float *ref_log, const float *advantage, const float *row_weights, double clip_low, double clip_high, double kl,
                       double scale, float *loss, float *log_prob, void *grad, int64_t ld_grad, void *stream);
@@ -441,15 +441,16 @@ int wpsgd_policy_loss(const void *Z, int64_t n, int64_t classes, int64_t ld, wps
  * both are -inf.  A label >= classes makes the pair's results NaN, and so does a score of a row that counts which is +inf or NaN.
  *   Z             DEVICE, n x classes, row stride ld elements, fp32 or bfloat16    labels  DEVICE, n
  *   offsets       DEVICE, 2 * pairs + 1 row numbers, none under the one before it, within 0 .. n.  Where a pair's three are not, its loss and margin are NaN, the
- *                 other pairs' are what they are without it, and nothing is said about the gradient (in place Z may hold the scores still).  (Rows that no sequence holds are read all the same, unless
- *                 their labels are negative.)
+ *                 other pairs' are what they are without it, and nothing is said about the gradient (in place Z may hold the scores
+ *                 still).  Rows that no sequence holds are read all the same, unless their labels are negative.
  *   ref_log       DEVICE, n fp32 (-loss of wpsgd_softmax_loss under a reference), or NULL for zeros
  *   row_weights   DEVICE, n fp32 (r_i), or NULL for ones         pair_weights  DEVICE, pairs fp32 (w_p), or NULL for ones
  *   loss, margin  DEVICE out, pairs fp32
  *   grad          DEVICE out, dtype as Z, row stride ld_grad; NULL: not wanted.  It may be Z itself (with ld_grad = ld), else it may not overlap it.
  *   workspace     DEVICE scratch of at least wpsgd_preference_loss_workspace(n, classes, pairs, dtype) bytes, 256-byte aligned
  *                 (may be NULL where that is 0)
- * Exponentials are fp32, their sums and sums over rows fp64; the result does not depend on timing.  Errors: INVALID_ARG (0 <= smoothing <= 1), WORKSPACE_TOO_SMALL, HIP_ERROR. */
+ * Exponentials are fp32, sums of more than eight of them and sums over rows fp64; the result does not depend on timing.  Errors: INVALID_ARG
+ * (0 <= smoothing <= 1), WORKSPACE_TOO_SMALL, HIP_ERROR. */
 size_t wpsgd_preference_loss_workspace(int64_t n, int64_t classes, int64_t pairs, wpsgd_dtype dtype);
 int wpsgd_preference_loss(const void *Z, int64_t n, int64_t classes, int64_t ld, wpsgd_dtype dtype, const int64_t *labels, const int64_t *offsets,
                           int64_t pairs, const float *ref_log, const float *row_weights, const float *pair_weights, wpsgd_loss kind, double beta,
@@ -488,7 +489,7 @@ typedef struct wpsgd_nibbles {
  * Errors: INVALID_ARG, UNSUPPORTED (CSR), HIP_ERROR. */
 int wpsgd_quantize_nibbles(const wpsgd_matrix *X, const int64_t *rows, int64_t n, const wpsgd_nibbles *out, void *stream);
 
-/* out[i*ld_out + j] = sum_c x(i, c) * W(j, c) for n rows of X (dense; CSR: UNSUPPORTED) and all rows j of W, made for few rows: every 64 of them read W once.  The values
+/* out[i*ld_out + j] = sum_c x(i, c) * W(j, c) for n rows of X (dense; CSR: UNSUPPORTED) and all rows j of W, made for few rows: every 64 of them read W once, or every 32 against few classes.  The values
  * of x are taken as they are (fp32 ones too), sums are fp32, rounded once to dtype.  A result that dtype holds comes out whatever the sizes of the elements; parts of fp32
  * elements under 2^-126, and less than 2^-116 of a group's sum of elements times codes and of a result, may be lost.
  *   rows   as for wpsgd_quantize       out   DEVICE, n x W->rows; it may not overlap X or W

@@ -213,7 +213,7 @@ struct Matmul4Args {
 // tile of sixteen rows is row 4 (i mod 4) + i / 4 of the instruction, so that up to four rows need one result register of a lane, up to eight two (R).  A group's products are summed by
 // themselves and times its scale added in fp32.  Of WAVES waves in a workgroup `along` share the sum, pairs of blocks in turn, and add up through LDS in their order; the others take the next
 // classes.  HELD: the rows lie in LDS as fragments, up to 128 KiB of the sum at a time, fp32 ones as three parts; else each wave asks for its own part of them.
-// 8 x 65536 x 4096 fp32 (LDS) 43 us, 3.2 TB/s of codes; 1 x 4096 x 4096 (each wave) 7.1, a launch and three trips to memory one behind the other (row number, row, sum);
+// 8 x 65536 x 4096 fp32 (LDS) 42 us, 3.2 TB/s of codes out of memory (38 where the caches still hold them); 1 x 4096 x 4096 (each wave) 7.1, a launch and three trips to memory one behind the other (row number, row, sum);
 // 64 x 65536 x 4096 68, 500 TFLOP/s (74 with 64 KiB of rows at a time): fragments from LDS and codes widened for four tiles of rows at a time.
 template <int MT, int R, int PARTS> constexpr int held_blocks4()
 {
@@ -511,7 +511,8 @@ __global__ __launch_bounds__(64 * WAVES) void matmul4_kernel(Matmul4Args g, int 
 // Up to sixteen rows of up to 4096 columns against many classes.  The waves of a workgroup hold the rows in registers, `along` waves a pair of blocks each; kStreamWaves / along of
 // them stand beside each other for other classes.  The classes' codes stream past, sixteen classes at a time, kBatch of those on their way, and every kBatch the waves' sums meet in
 // LDS, in their order.  fp32 rows are three rows of bfloat16 parts each, which the last addition puts together.
-// 16 x 65536 x 4096, groups of 32: 36 us, 4.3 TB/s; of 128: 33.5, 4.2; 1 x 65536 x 4096 28.3, 4.9.  Reading the codes alone takes 22 (6.1 TB/s).  The rest: codes and rows come in cold for some 8 us
+// 16 x 65536 x 4096, groups of 32: 36 us, 4.3 TB/s; of 128: 33, 4.2; 1 x 65536 x 4096 28, 4.9 (several class matrices in turn, so that codes come out of memory; the same one again
+// and again: 30, 28.5 and 25.6).  Reading the codes alone takes 22, at the 6.1 to 6.4 TB/s that reading alone reaches.  The rest: codes and rows come in cold for some 8 us
 // before the first results (each kernel also reads its own instructions, one line behind the other: the way through the start is kept short), and the waves wait for each other at the
 // end.  Batches of four tiles: 35 us for the first of these, but 1 x 65536 x 4096 29.4 and 4 x 16384 x 4096 12.7 instead of 11.5: twice the instructions.
 constexpr int kStreamWaves = 16, kBatch = 2;
@@ -717,7 +718,8 @@ static hipError_t launch_matmul4(const Matmul4Args &g, hipStream_t s)
     // wave: 1 x 65536 x 4096 28.3 | 34.0 | 45.5, 16 x 65536 x 4096 33.5 | 35.8 | 85.6, 4 x 16384 x 4096 11.5 | 15.6 | 14.9; 1 x 4096 x 4096, one tile a workgroup, 11.1 | 14.1 | 7.1).
     if (rows <= 16 && pairs <= 16 && tiles * along > 256 * 16) return rows <= 4 ? launch_stream<1, G>(g, along, s) : launch_stream<4, G>(g, along, s);
     // Rows in LDS where many classes share them, else asked for by each wave (us, in LDS | by each wave: 64 x 65536 x 4096 68 | 169 bfloat16, 143 | 286 fp32; 256 x 16384 x 4096 61 | 167;
-    // 64 x 16384 x 4096 44 | 46, 133 | 75 fp32; 37 x 5003 x 3001 fp32 92 | 18; 20 x 20000 x 1000 fp32 22.7 | 24.6; 8 x 65536 x 4096 fp32 43 | 92).
+    // 64 x 16384 x 4096 44 | 46, 133 | 75 fp32; 37 x 5003 x 3001 fp32 92 | 18; 20 x 20000 x 1000 fp32 22.7 | 24.6; 8 x 65536 x 4096 fp32 43 | 92).  The few percent lost
+    // at 64 x 16384 x 4096 bfloat16 and 20 x 20000 x 1000 fp32 are the price of one number for both types.
     if (g.n <= 16 ? tiles > 1024 : tiles * ((g.n + 63) / 64) >= 2048) {
         if (g.n <= 8) return launch_rows<T, 1, 2, 1, G, 16, true>(g, s);
         if (g.n <= 16) return launch_rows<T, 1, 4, 1, G, 16, true>(g, s);

@@ -5,7 +5,8 @@
 //   grad_ic = f_i (softmax(z_i)_c - [c = label_i]),  f_i = -+ scale beta r_i w_p ((1 - eps) L'(h_p) - eps L'(-h_p)).
 // A row's gradient waits for its whole pair, so the scores are read twice: row_softmax.h's pass leaves each row's statistics and g_i, a workgroup a pair adds those up (in fp64,
 // in an order that depends on the lengths alone) and leaves each row's f_i, and the last pass forms the gradient.  16 pairs of some 512 rows of 65536 bfloat16 scores: 197 us, 5.1 and 393, all
-// of it memory, 5.4 TB/s of the three passes' 3.2 GB.  The second reading costs no less out of the caches: rows of 64 to 256 MB at a time take the same time each as 1 GB (the gradient's writes bound it).
+// of it memory, 5.4 TB/s of the three passes' 3.2 GB (reading alone reaches 6.4 TB/s on this card, writing alone 6.8 to 7.5, one beside the other the last pass's 5.4).  A pair at a time, whose
+// 64 MB the Infinity Cache still holds for the second reading, the last passes take 365 us together, the first ones 420 instead of 197: too short to fill the card.
 #include "row_softmax.h"
 
 namespace wpsgd {
